@@ -353,6 +353,96 @@ enum { SAMKV_OVERWRITE = 0, SAMKV_FUSION = 1 };
 int samkv_kv_update(void* k_c, void* v_c, const void* k_new, const void* v_new, int32_t m_total,
                     int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t mode, void* stream);
 
+/* ---- Prompts in, answers out: packed prefill, and a paged cache that grows token by token -----------------------------
+ *
+ * What a serving program does before and after the sparse path above: documents and prompts are prefilled (each for
+ * itself, several in one batch), keys and values are kept in pages, and new tokens attend over them.  Conventions as above,
+ * except that
+ *   - attention outputs are in `dtype`, rounded once at the end: what the next projection takes;
+ *   - tensors of rows (samkv_rows) have strides: element (head h, row t, channel c) lies at
+ *     p + h * head_stride + t * row_stride + c, strides in elements, non-negative and multiples of 16 bytes.  So the queries,
+ *     keys and values may be views of one projection's output [tokens][Hq + 2 Hkv][d], or [heads][tokens][d].  Rows that are
+ *     written must not overlap (SAMKV_EINVAL); rows that are only read may (a stride of 0 repeats a row);
+ *   - lengths, prefix sums and page tables are DEVICE arrays, so that a captured graph can be replayed while a batch grows.
+ *     The host passes bounds for them (max_len, max_new).  Whatever the arrays hold, no access leaves the tensors: a
+ *     length beyond its bound counts as the bound, a negative one as zero, a sequence's rows end at the tensors' last row, and
+ *     page numbers outside [0, n_pages) are taken as the nearest page when they are read and not written to at all.
+ *     Sequences are packed one behind the other; rows behind the last one are neither read nor written. */
+#define SAMKV_MAX_SEQ 4096
+typedef struct {
+  void* p;
+  int64_t head_stride, row_stride;
+} samkv_rows;
+
+/* The pages of one layer: k, v device [n_pages][n_kv_heads][page_size][head_dim].  page_size is a power of two from 16 to
+ * 1024.  n_pages has no bound but memory: positions are 64-bit.  Host struct. */
+typedef struct {
+  int32_t n_pages, page_size, n_kv_heads, head_dim, dtype;
+  void* k;
+  void* v;
+} samkv_pages;
+
+/* A batch of sequences with their newest tokens.  Sequence s holds len[s] tokens INCLUDING its new ones, which are rows
+ * cu_new[s] .. cu_new[s + 1] - 1 of the batch's tensors and take the last of its slots.  Slot p of sequence s is row
+ * p % page_size of page table[s][p / page_size].  A new token before slot 0 (more new tokens than len) has no slot.
+ * Pages may be shared between sequences (a common prefix).  Host struct. */
+typedef struct {
+  int32_t n_seq;          /* 1 .. SAMKV_MAX_SEQ */
+  int32_t max_pages;      /* columns of table */
+  int32_t max_len;        /* no len[s] counts beyond this; at most max_pages * page_size */
+  int32_t max_new;        /* no sequence has more new tokens that count */
+  int32_t n_new;          /* rows of the batch's tensors */
+  const int32_t* table;   /* device [n_seq][max_pages] */
+  const int32_t* len;     /* device [n_seq] */
+  const int32_t* cu_new;  /* device [n_seq + 1], from 0 ascending; NULL: every sequence has max_new, n_new = n_seq * max_new */
+} samkv_batch;
+
+/* Rotary position embedding of the first rot_dim channels (a multiple of 16, at most head_dim): pair i is turned by
+ * pos * inv_freq[i], pairs are channels (i, i + rot_dim / 2), or (2 i, 2 i + 1) when interleaved.  Host struct. */
+typedef struct {
+  const float* inv_freq;     /* device [rot_dim / 2] */
+  int32_t rot_dim, interleaved;
+  const int32_t* positions;  /* device [n_new], or NULL: a token's position is its slot */
+} samkv_rope;
+
+/* Causal attention of packed prompts, each for itself: row t of sequence s attends to its rows 0..t.
+ *   out[h][t][:] = sum_{j <= t} softmax_j(scale * <q[h][t], k[g][j]>) * v[g][j],  lse[h][t] = log sum_{j <= t} exp(...)
+ *   q, out  n_q_heads of n_tok rows, k, v  n_kv_heads of n_tok rows (out and k, v in dtype); lse float32 [n_q_heads][n_tok], may
+ *   be NULL.  cu  device [n_seq + 1]: sequence s is rows cu[s] .. cu[s + 1] - 1.  max_len: bound of the sequences' lengths, rows
+ *   of a longer one past the bound are left as they were.
+ * This is the prefill that gives the per-document caches of samkv_caches.  Keys and values of later rows do not reach a row
+ * whatever they hold (infinities and NaN included).
+ * Arithmetic: float32 scores, statistics and sums.
+ * ws: samkv_prefill_workspace_bytes(...) bytes, 256-byte aligned. */
+size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t dtype);
+int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_rows* v, const int32_t* cu, int32_t n_seq,
+                       int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                       float scale, const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Keys and values of a batch's new tokens into their slots, K rotated on the way, and the queries beside them.
+ *   k_new, v_new  n_kv_heads of n_new rows, in the pages' dtype
+ *   rope          NULL: nothing is rotated (keys that come rotated, as a compacted cache's do)
+ *   q, q_out      n_q_heads of n_new rows, in the pages' dtype, q_out = q rotated; both NULL: no queries.  q_out may be q
+ *                 itself (same address and strides); otherwise what is written must not overlap what is read.
+ * Angles are reduced in float64, the rotation is float32 and rounded once.  A token without a slot, or whose page number is
+ * outside [0, n_pages), is not written (its query still is rotated, by its given position, or else by 0).  Two sequences that
+ * write to one row of a shared page leave either's. */
+int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* k_new, const samkv_rows* v_new,
+                       const samkv_rope* rope, const samkv_rows* q, const samkv_rows* q_out, int32_t n_q_heads, void* stream);
+
+/* Attention of a batch's new tokens over its paged cache, which holds their own keys and values already: the token at slot p
+ * attends to slots 0..p of its sequence.
+ *   out[h][t][:] = sum_{j <= p} softmax_j(scale * <q[h][t], K_j[g]>) * V_j[g],  lse[h][t] = log sum_{j <= p} exp(...)
+ *   q, out  n_q_heads of n_new rows in the pages' dtype; lse float32 [n_q_heads][n_new], may be NULL.
+ * One new token per sequence is a decoding step; several are drafted tokens or a chunk of a prompt; both mix in one batch.
+ * A token without a slot attends to nothing: out 0, lse -inf.  Slots behind a token do not reach it whatever they hold.
+ * Arithmetic as in samkv_prefill_attn.
+ * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned. */
+size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads);
+int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
+                     const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 /* Diagnostics, not part of the method: two micro-kernels with which a benchmark measures what this device
  * sustains, to quote kernel rates against the measured ceiling as well as the published one.  The caller times the
  * launch (HIP events on `stream`).

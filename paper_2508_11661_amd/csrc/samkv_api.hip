@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "common.hpp"
+#include "paged.hpp"
 
 using namespace samkv;
 
@@ -967,6 +968,145 @@ int samkv_kv_update(void* k_c, void* v_c, const void* k_new, const void* v_new, 
   a.n_rows = (long long)m_total * n_kv_heads;
   a.k_cur = k_c; a.v_cur = v_c; a.k_new = k_new; a.v_new = v_new;
   return dev(launch_kv_update(a, static_cast<hipStream_t>(stream)));
+}
+
+// ---- packed prompts and paged caches ----
+
+// Rows of `heads` heads that a kernel reads or writes (`written`: no two of them may share memory).
+static int check_rows(const samkv_rows* r, int heads, int rows, int d, int dtype, bool written, RowsArg* out) {
+  if (r == nullptr || r->p == nullptr || !aligned16(r->p)) return SAMKV_EINVAL;
+  const int e = dtype == SAMKV_BF16 ? 2 : 4;
+  const long long hs = r->head_stride, rs = r->row_stride;
+  if (hs < 0 || rs < 0 || hs * e % 16 != 0 || rs * e % 16 != 0) return SAMKV_EINVAL;
+  if (hs > (1ll << 58) / heads || rs > (1ll << 58) / rows) return SAMKV_EUNSUPPORTED;  // offsets in bytes stay below 2^63
+  if (written) {
+    const bool head_major = hs >= (rows - 1) * rs + d && (rows == 1 || rs >= d);
+    const bool row_major = rs >= (heads - 1) * hs + d && (heads == 1 || hs >= d);
+    if (!(heads == 1 && (rows == 1 || rs >= d)) && !(rows == 1 && (heads == 1 || hs >= d)) && !head_major && !row_major)
+      return SAMKV_EINVAL;
+  }
+  out->p = static_cast<char*>(r->p);
+  out->hs = hs * e;
+  out->rs = rs * e;
+  return SAMKV_OK;
+}
+
+static int check_heads(int hq, int hkv, int d, int dtype) {
+  if (hq < 1 || hkv < 1 || hq % hkv != 0) return SAMKV_EINVAL;
+  if ((dtype != SAMKV_F32 && dtype != SAMKV_BF16) || (d != 64 && d != 128)) return SAMKV_EUNSUPPORTED;
+  return hq > 65535 ? SAMKV_EUNSUPPORTED : SAMKV_OK;
+}
+
+static int check_batch(const samkv_pages* pages, const samkv_batch* batch, int hq, BatchArg* b) {
+  if (pages == nullptr || batch == nullptr || pages->k == nullptr || pages->v == nullptr) return SAMKV_EINVAL;
+  if (!aligned16(pages->k) || !aligned16(pages->v) || pages->n_pages < 1) return SAMKV_EINVAL;
+  const int rc = check_heads(hq, pages->n_kv_heads, pages->head_dim, pages->dtype);
+  if (rc != SAMKV_OK) return rc;
+  const int size = pages->page_size;
+  if (size < 1) return SAMKV_EINVAL;
+  if (size < 16 || size > 1024 || (size & (size - 1)) != 0) return SAMKV_EUNSUPPORTED;
+  if (batch->table == nullptr || batch->len == nullptr || (uintptr_t)batch->table % 4 != 0 || (uintptr_t)batch->len % 4 != 0 ||
+      (uintptr_t)batch->cu_new % 4 != 0)
+    return SAMKV_EINVAL;
+  if (batch->n_seq < 1 || batch->max_pages < 1 || batch->max_len < 1 || batch->max_new < 1 || batch->n_new < 1) return SAMKV_EINVAL;
+  if (batch->max_len > (long long)batch->max_pages * size) return SAMKV_EINVAL;
+  if (batch->cu_new == nullptr && (long long)batch->n_seq * batch->max_new != batch->n_new) return SAMKV_EINVAL;
+  if (batch->n_seq > SAMKV_MAX_SEQ || batch->max_len > 0x7FFFFFFF / 4 || (long long)hq * batch->n_new > 0x7FFFFFFF / 256)
+    return SAMKV_EUNSUPPORTED;
+  b->n_seq = batch->n_seq; b->n_rows = batch->n_new; b->max_len = batch->max_len;
+  b->max_new = batch->max_new < batch->n_new ? batch->max_new : batch->n_new;
+  b->cu = batch->cu_new; b->len = batch->len; b->table = batch->table;
+  b->max_pages = batch->max_pages; b->n_pages = pages->n_pages;
+  b->page_log2 = __builtin_ctz((unsigned)size);
+  return SAMKV_OK;
+}
+
+static int check_prompts(int n_seq, int n_tok, int max_len, int hq, int hkv, int d, int dtype) {
+  const int rc = check_heads(hq, hkv, d, dtype);
+  if (rc != SAMKV_OK) return rc;
+  if (n_seq < 1 || n_tok < 1 || max_len < 1) return SAMKV_EINVAL;
+  return n_seq > SAMKV_MAX_SEQ || (long long)hq * n_tok > 0x7FFFFFFF / 256 ? SAMKV_EUNSUPPORTED : SAMKV_OK;
+}
+
+static bool bad_lse(const float* lse) { return (uintptr_t)lse % 4 != 0; }
+
+size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads,
+                                     int32_t head_dim, int32_t dtype) {
+  if (check_prompts(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype) != SAMKV_OK) return 0;
+  const int most = max_len < n_tok ? max_len : n_tok;
+  return paged_attn_ws_bytes(dtype, head_dim, n_q_heads, n_kv_heads, n_seq, n_tok, most, most);
+}
+
+int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_rows* v, const int32_t* cu, int32_t n_seq,
+                       int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                       float scale, const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_prompts(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype);
+  if (rc != SAMKV_OK) return rc;
+  if (cu == nullptr || (uintptr_t)cu % 4 != 0 || bad_lse(lse) || !(scale > 0.f) || !isfinite(scale)) return SAMKV_EINVAL;
+  PagedAttnLaunch a;
+  memset(&a, 0, sizeof(a));
+  if ((rc = check_rows(q, n_q_heads, n_tok, head_dim, dtype, false, &a.q)) != SAMKV_OK) return rc;
+  if ((rc = check_rows(k, n_kv_heads, n_tok, head_dim, dtype, false, &a.k)) != SAMKV_OK) return rc;
+  if ((rc = check_rows(v, n_kv_heads, n_tok, head_dim, dtype, false, &a.v)) != SAMKV_OK) return rc;
+  if ((rc = check_rows(out, n_q_heads, n_tok, head_dim, dtype, true, &a.out)) != SAMKV_OK) return rc;
+  const size_t need = samkv_prefill_workspace_bytes(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype);
+  if (!enough(ws, ws_bytes, need)) return SAMKV_EWORKSPACE;
+  a.dtype = dtype; a.d = head_dim; a.hq = n_q_heads; a.hkv = n_kv_heads; a.paged = 0;
+  a.b.n_seq = n_seq; a.b.n_rows = n_tok; a.b.max_new = a.b.max_len = max_len < n_tok ? max_len : n_tok;
+  a.b.cu = cu;
+  a.lse = lse; a.scale = scale; a.ws = ws;
+  return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
+}
+
+int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* k_new, const samkv_rows* v_new,
+                       const samkv_rope* rope, const samkv_rows* q, const samkv_rows* q_out, int32_t n_q_heads, void* stream) {
+  AppendLaunch a;
+  memset(&a, 0, sizeof(a));
+  const bool with_q = q != nullptr || q_out != nullptr;
+  int rc = check_batch(pages, batch, with_q ? n_q_heads : pages != nullptr ? pages->n_kv_heads : 0, &a.b);
+  if (rc != SAMKV_OK) return rc;
+  const int d = pages->head_dim, dtype = pages->dtype, n = batch->n_new;
+  if ((rc = check_rows(k_new, pages->n_kv_heads, n, d, dtype, false, &a.k_new)) != SAMKV_OK) return rc;
+  if ((rc = check_rows(v_new, pages->n_kv_heads, n, d, dtype, false, &a.v_new)) != SAMKV_OK) return rc;
+  if (with_q) {
+    if ((rc = check_rows(q, n_q_heads, n, d, dtype, false, &a.q)) != SAMKV_OK) return rc;
+    if ((rc = check_rows(q_out, n_q_heads, n, d, dtype, true, &a.q_out)) != SAMKV_OK) return rc;
+    a.hq = n_q_heads;
+  }
+  if (rope != nullptr) {
+    if (rope->inv_freq == nullptr || (uintptr_t)rope->inv_freq % 4 != 0 || (uintptr_t)rope->positions % 4 != 0) return SAMKV_EINVAL;
+    if (rope->rot_dim < 1 || rope->rot_dim > d || rope->rot_dim % 2 != 0) return SAMKV_EINVAL;
+    if (rope->rot_dim % 16 != 0) return SAMKV_EUNSUPPORTED;
+    a.inv_freq = rope->inv_freq; a.rot = rope->rot_dim; a.interleaved = rope->interleaved != 0; a.positions = rope->positions;
+  }
+  a.dtype = dtype; a.d = d; a.hkv = pages->n_kv_heads;
+  a.k = static_cast<char*>(pages->k); a.v = static_cast<char*>(pages->v);
+  return dev(launch_paged_append(a, static_cast<hipStream_t>(stream)));
+}
+
+size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads) {
+  BatchArg b;
+  if (check_batch(pages, batch, n_q_heads, &b) != SAMKV_OK) return 0;
+  return paged_attn_ws_bytes(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new, b.max_len);
+}
+
+int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
+                     const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  PagedAttnLaunch a;
+  memset(&a, 0, sizeof(a));
+  int rc = check_batch(pages, batch, n_q_heads, &a.b);
+  if (rc != SAMKV_OK) return rc;
+  if (bad_lse(lse) || !(scale > 0.f) || !isfinite(scale)) return SAMKV_EINVAL;
+  const int d = pages->head_dim, dtype = pages->dtype, e = dtype == SAMKV_BF16 ? 2 : 4;
+  if ((rc = check_rows(q, n_q_heads, batch->n_new, d, dtype, false, &a.q)) != SAMKV_OK) return rc;
+  if ((rc = check_rows(out, n_q_heads, batch->n_new, d, dtype, true, &a.out)) != SAMKV_OK) return rc;
+  if (!enough(ws, ws_bytes, samkv_paged_workspace_bytes(pages, batch, n_q_heads))) return SAMKV_EWORKSPACE;
+  a.dtype = dtype; a.d = d; a.hq = n_q_heads; a.hkv = pages->n_kv_heads; a.paged = 1;
+  a.k.p = static_cast<char*>(pages->k); a.v.p = static_cast<char*>(pages->v);
+  a.k.rs = a.v.rs = d * e;
+  a.k.hs = a.v.hs = (long long)pages->page_size * d * e;
+  a.lse = lse; a.scale = scale; a.ws = ws;
+  return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,4 +1,4 @@
-"""ctypes binding of libsamkv.so: the same five entry points as include/samkv.h, taking torch tensors.
+"""ctypes binding of libsamkv.so: the same entry points as include/samkv.h, taking torch tensors.
 
 Argument marshalling only: every step of the path runs in the HIP kernels of the library.  torch is
 used for device memory and for the current stream.  If the library is missing the import of this
@@ -22,7 +22,8 @@ EXPORTS = ("samkv_strerror", "samkv_kept_count", "samkv_kept_count_mid", "samkv_
            "samkv_gather_q_v", "samkv_block_scores", "samkv_block_workspace_bytes", "samkv_block_select",
            "samkv_block_select_filter", "samkv_block_filter_count", "samkv_block_select_count", "samkv_gather_g", "samkv_gather_q_g",
            "samkv_gather", "samkv_gather_q", "samkv_recompute_attn", "samkv_query_attn", "samkv_recompute_query_attn", "samkv_hot_path", "samkv_query_attn_self",
-           "samkv_kv_update", "samkv_peak_mfma_bf16", "samkv_peak_mfma_bf16_data", "samkv_peak_copy", "samkv_peak_read")
+           "samkv_kv_update", "samkv_prefill_workspace_bytes", "samkv_prefill_attn", "samkv_paged_append",
+           "samkv_paged_workspace_bytes", "samkv_paged_attn", "samkv_peak_mfma_bf16", "samkv_peak_mfma_bf16_data", "samkv_peak_copy", "samkv_peak_read")
 SAMKV_OVERWRITE, SAMKV_FUSION = 0, 1
 
 
@@ -33,6 +34,26 @@ class _Caches(ctypes.Structure):
         ("len", ctypes.POINTER(ctypes.c_int32)),
         ("k", ctypes.POINTER(ctypes.c_void_p)), ("v", ctypes.POINTER(ctypes.c_void_p)),
     ]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("n_new", ctypes.c_int32), ("table", ctypes.c_void_p), ("len", ctypes.c_void_p),
+                ("cu_new", ctypes.c_void_p)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("positions", ctypes.c_void_p)]
 
 
 def _load() -> ctypes.CDLL:
@@ -106,6 +127,17 @@ def _load() -> ctypes.CDLL:
     lib.samkv_peak_copy.argtypes = [vp, vp, sz, vp]
     lib.samkv_peak_read.restype = ctypes.c_int
     lib.samkv_peak_read.argtypes = [vp, sz, vp, vp]
+    rows, pages, batch = ctypes.POINTER(_Rows), ctypes.POINTER(_Pages), ctypes.POINTER(_Batch)
+    lib.samkv_prefill_workspace_bytes.restype = sz
+    lib.samkv_prefill_workspace_bytes.argtypes = [i32] * 7
+    lib.samkv_prefill_attn.restype = ctypes.c_int
+    lib.samkv_prefill_attn.argtypes = [rows, rows, rows, vp, i32, i32, i32, i32, i32, i32, i32, f32, rows, vp, vp, sz, vp]
+    lib.samkv_paged_append.restype = ctypes.c_int
+    lib.samkv_paged_append.argtypes = [pages, batch, rows, rows, ctypes.POINTER(_Rope), rows, rows, i32, vp]
+    lib.samkv_paged_workspace_bytes.restype = sz
+    lib.samkv_paged_workspace_bytes.argtypes = [pages, batch, i32]
+    lib.samkv_paged_attn.restype = ctypes.c_int
+    lib.samkv_paged_attn.argtypes = [pages, batch, rows, i32, f32, rows, vp, vp, sz, vp]
     lib.samkv_kv_update.restype = ctypes.c_int
     lib.samkv_kv_update.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, i32, vp]
     return lib
@@ -477,6 +509,131 @@ def samkv_kv_update(k_c: torch.Tensor, v_c: torch.Tensor, k_new: torch.Tensor, v
         assert t.shape == k_c.shape and t.dtype == k_c.dtype
     _check(_lib.samkv_kv_update(_ptr(k_c), _ptr(v_c), _ptr(k_new), _ptr(v_new), m, hkv, d, _dtype_code(k_c.dtype),
                                 mode, _stream()), "samkv_kv_update")
+
+
+# ------------------------------------------------------------------------------------------------
+# Packed prompts and paged caches.  Row tensors are [heads, tokens, d] with a dense last dimension and any strides of
+# multiples of 16 bytes before it (a transposed view of a projection's [tokens, heads, d] output, say).
+def _current_device() -> int:
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _rows(t: torch.Tensor, heads: int, n: int, d: int, dtype: torch.dtype, device: int) -> _Rows:
+    assert tuple(t.shape) == (heads, n, d), f"{tuple(t.shape)} instead of {(heads, n, d)}"
+    assert t.dtype == dtype and t.is_cuda and t.get_device() == device, "dtype or device of a row tensor"
+    s = t.stride()
+    assert s[2] == 1, "the last dimension must be dense"
+    return _Rows(t.data_ptr(), s[0] if heads > 1 else 0, s[1] if n > 1 else 0)
+
+
+def _int32(t: torch.Tensor, n: int, device: int) -> int:
+    assert t.dtype == torch.int32 and t.is_cuda and t.get_device() == device and t.is_contiguous() and t.numel() == n
+    return t.data_ptr()
+
+
+def _lse(t: Optional[torch.Tensor], heads: int, n: int, device: int) -> Optional[int]:
+    if t is None:
+        return None
+    assert t.dtype == torch.float32 and tuple(t.shape) == (heads, n) and t.is_contiguous() and t.get_device() == device
+    return t.data_ptr()
+
+
+def _scratch(ws: Optional[torch.Tensor], device: int) -> Tuple[Optional[int], int]:
+    if ws is None:
+        return None, 0
+    assert ws.is_contiguous() and ws.get_device() == device
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+class PagedCache:
+    """K and V pages of one layer: k, v [n_pages, Hkv, page_size, d] device tensors."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        assert k.is_cuda and k.dim() == 4 and k.is_contiguous() and v.is_contiguous()
+        assert v.shape == k.shape and v.dtype == k.dtype and v.device == k.device
+        self.k, self.v, self.device = k, v, k.get_device()
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
+        self.c = _Pages(self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _dtype_code(k.dtype), k.data_ptr(),
+                        v.data_ptr())
+
+
+class PagedBatch:
+    """The sequences of a batch: table [n_seq, max_pages], lens [n_seq] (tokens, the new ones included) and cu_new [n_seq + 1]
+    (prefix sums of the new tokens; None: max_new in every sequence), int32 device tensors that may change between calls.
+    max_len and max_new are bounds, n_new the rows of the batch's tensors."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, max_len: int, cu_new: Optional[torch.Tensor] = None,
+                 max_new: int = 1, n_new: Optional[int] = None):
+        assert table.is_cuda and table.dim() == 2
+        n_seq, max_pages = table.shape
+        self.device = table.get_device()
+        self.n_new = n_seq * max_new if n_new is None else n_new
+        self.table, self.lens, self.cu_new = table, lens, cu_new
+        self.c = _Batch(n_seq, max_pages, max_len, max_new, self.n_new, _int32(table, n_seq * max_pages, self.device),
+                        _int32(lens, n_seq, self.device), None if cu_new is None else _int32(cu_new, n_seq + 1, self.device))
+
+
+class Rope:
+    """Rotary position embedding: pair i of the first 2 * len(inv_freq) channels is turned by position * inv_freq[i].
+    positions: int32 [n_new], or None: every token's slot."""
+
+    def __init__(self, inv_freq: torch.Tensor, interleaved: bool = False, positions: Optional[torch.Tensor] = None):
+        assert inv_freq.is_cuda and inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous()
+        self.inv_freq, self.positions, self.device = inv_freq, positions, inv_freq.get_device()
+        self.c = _Rope(inv_freq.data_ptr(), 2 * inv_freq.numel(), int(interleaved),
+                       None if positions is None else _int32(positions, positions.numel(), self.device))
+
+
+def samkv_prefill_workspace_bytes(n_seq: int, n_tok: int, max_len: int, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                                  dtype: torch.dtype) -> int:
+    return int(_lib.samkv_prefill_workspace_bytes(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, _dtype_code(dtype)))
+
+
+def samkv_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, max_len: int, scale: float,
+                       out: torch.Tensor, lse: Optional[torch.Tensor], ws: Optional[torch.Tensor]) -> None:
+    """out [Hq, T, d] in the inputs' dtype, lse [Hq, T] float32 <- causal attention of packed prompts, cu [n_seq + 1] int32."""
+    dev = _current_device()
+    hq, n, d = q.shape
+    hkv, dt = k.shape[0], q.dtype
+    n_seq = cu.numel() - 1
+    p, n_bytes = _scratch(ws, dev)
+    _check(_lib.samkv_prefill_attn(_rows(q, hq, n, d, dt, dev), _rows(k, hkv, n, d, dt, dev), _rows(v, hkv, n, d, dt, dev),
+                                   _int32(cu, n_seq + 1, dev), n_seq, n, max_len, hq, hkv, d, _dtype_code(dt), scale,
+                                   _rows(out, hq, n, d, dt, dev), _lse(lse, hq, n, dev), p, n_bytes, _stream()),
+           "samkv_prefill_attn")
+
+
+def samkv_paged_append(cache: PagedCache, batch: PagedBatch, k_new: torch.Tensor, v_new: torch.Tensor,
+                       rope: Optional[Rope] = None, q: Optional[torch.Tensor] = None,
+                       q_out: Optional[torch.Tensor] = None) -> None:
+    """Pages <- k_new (rotated), v_new [Hkv, n_new, d]; q_out [Hq, n_new, d] <- q rotated (q_out may be q)."""
+    dev = _current_device()
+    assert cache.device == batch.device == dev
+    n, d, dt = batch.n_new, cache.head_dim, cache.k.dtype
+    if rope is not None:
+        assert rope.device == dev and (rope.positions is None or rope.positions.numel() == n)
+    hq = 0 if q is None else q.shape[0]
+    _check(_lib.samkv_paged_append(cache.c, batch.c, _rows(k_new, cache.n_kv_heads, n, d, dt, dev),
+                                   _rows(v_new, cache.n_kv_heads, n, d, dt, dev), None if rope is None else rope.c,
+                                   None if q is None else _rows(q, hq, n, d, dt, dev),
+                                   None if q_out is None else _rows(q_out, hq, n, d, dt, dev), hq, _stream()),
+           "samkv_paged_append")
+
+
+def samkv_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_q_heads: int) -> int:
+    return int(_lib.samkv_paged_workspace_bytes(cache.c, batch.c, n_q_heads))
+
+
+def samkv_paged_attn(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: float, out: torch.Tensor,
+                     lse: Optional[torch.Tensor], ws: Optional[torch.Tensor]) -> None:
+    """out [Hq, n_new, d] in the cache's dtype, lse [Hq, n_new] float32 <- attention of the new tokens over the pages."""
+    dev = _current_device()
+    assert cache.device == batch.device == dev
+    hq, n, d = q.shape[0], batch.n_new, cache.head_dim
+    dt = cache.k.dtype
+    p, n_bytes = _scratch(ws, dev)
+    _check(_lib.samkv_paged_attn(cache.c, batch.c, _rows(q, hq, n, d, dt, dev), hq, scale, _rows(out, hq, n, d, dt, dev),
+                                 _lse(lse, hq, n, dev), p, n_bytes, _stream()), "samkv_paged_attn")
 
 
 # ------------------------------------------------------------------------------------------------
