@@ -977,7 +977,8 @@ hipError_t attn_prepare_device() {
   if (done[dev]) return hipSuccess;
   const hipError_t all[] = {
       raise_lds_limit<128>(), raise_lds_limit<64>(), raise_lds_limit_dma<128, 2, 1>(), raise_lds_limit_dma<64, 2, 2>(),
-      raise_lds_limit_dma<64, 2, 1>(), raise_lds_limit_dma<128, 1, 1>(), raise_lds_limit_dma<64, 1, 2>(), attn_f32_raise_limits()};
+      raise_lds_limit_dma<64, 2, 1>(), raise_lds_limit_dma<128, 1, 1>(), raise_lds_limit_dma<64, 1, 2>(), attn_f32_raise_limits(),
+      paged_attn_raise_limits()};
   for (hipError_t x : all)
     if (x != hipSuccess) return x;
   done[dev] = true;

@@ -234,7 +234,8 @@ hipError_t launch_attn_f32(const AttnLaunch& a, hipStream_t s);
 // Both float32 attentions in one launch (the query attention's key chunks as in its own launch; the merge, where there
 // is one, stays a launch of its own).
 hipError_t launch_attn_f32_pair(const AttnLaunch& causal, const AttnLaunch& query, hipStream_t s);
-hipError_t attn_f32_raise_limits();  // part of attn_prepare_device
+hipError_t attn_f32_raise_limits();  // part of attn_prepare_device, as is
+hipError_t paged_attn_raise_limits();
 constexpr int kMaxParts = 64;  // partial results that one merge takes: key chunks and, for query_attn_self, the own keys
 hipError_t launch_attn_merge(const AttnLaunch& a, hipStream_t s);
 

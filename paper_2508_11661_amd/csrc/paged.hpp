@@ -58,6 +58,13 @@ struct AppendLaunch {
 hipError_t launch_paged_append(const AppendLaunch& a, hipStream_t s);
 
 // Attention of the rows of a batch over prompts (k and v as rows) or over pages.
+//
+// How a batch becomes workgroups.  The rows of a sequence that read one KV head are its tokens' query heads of that group,
+// token by token (row t G + g), cut into tiles; the keys that a tile sees are cut into chunks of `chunk` keys, whose partial
+// results a second kernel joins.  A work item is (sequence, tile, chunk), a workgroup one item of one KV head.  The grid has
+// room for every batch within the host's bounds; which item a workgroup takes, and how long a chunk is, every wave finds from
+// the lengths (find_item): the keys of all tiles are shared out over as many workgroups as are wanted (`target`), so that a
+// long sequence among short ones does not hold up the batch.
 struct PagedAttnLaunch {
   int dtype, d, hq, hkv, paged;
   BatchArg b;
@@ -65,9 +72,20 @@ struct PagedAttnLaunch {
   RowsArg k, v;  // pages: hs = bytes of one head's rows of a page, rs = bytes of a row
   float* lse;    // may be null
   float scale;
-  void* ws;
+  int target, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys
+  int max_items;          // items there is room for
+  int tile_rows;          // rows of a tile that partial results have room for
+  float* part_o;          // [max_items][hkv][tile_rows][d], normalised
+  float* part_lse;        // [max_items][hkv][tile_rows], in units of log 2
 };
 hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
-size_t paged_attn_ws_bytes(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len);
+
+// Sizes of a launch that follow from the bounds alone.
+struct PagedAttnPlan {
+  int target, min_chunk, max_tiles, max_items, tile_rows;
+  bool joins;  // whether any sequence can have more than one chunk
+  size_t part_lse, bytes;  // workspace: part_o, then part_lse
+};
+PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged);
 
 }  // namespace samkv

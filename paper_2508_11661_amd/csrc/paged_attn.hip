@@ -1,13 +1,365 @@
 // Attention of the rows of a batch of sequences over packed prompts (samkv_prefill_attn) or over pages (samkv_paged_attn):
-// the row at slot p of its sequence sees slots 0..p.
-// One wave per (row, query head): a lane scores one key of 64, the wave's maximum and sum run along, and every lane then
-// adds the weighted values of its own channels.
-#include "attn_common.hpp"
-#include "paged.hpp"
+// the row at slot p of its sequence sees slots 0..p.  bf16; float32: paged_attn_f32.hip.
+//
+// Products as in attn.hip: S^T = K Q^T and O^T += V^T P^T with v_mfma_f32_32x32x16_bf16, a wave holding 32 rows in its lanes'
+// columns, so that the softmax weights come out of the first product in the operand layout of the second and V is turned by
+// the transposing LDS read.
+#include <mutex>
+
+#include "paged_attn.hpp"
 
 namespace samkv {
 namespace {
 
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// ---------------------------------------------------------------------------------------------- few rows
+// A workgroup is NW waves that share one tile of 32 rows and split the keys of their chunk: wave w takes tiles of BK keys w, w
+// + NW, ...  Each wave has its own K and V slot in LDS, filled by asynchronous loads one tile ahead of their use (K of the next
+// tile is requested as soon as K's fragments are in registers, V likewise), so there is no barrier until the waves' results are
+// joined.
+template <int D, int NW>
+struct FewCfg {
+  static constexpr int ROWB = D * 2, CPR = ROWB / 16, RPI = 1024 / ROWB;  // bytes and chunks per row, rows per request
+  static constexpr int BK = 8192 / ROWB, NI = 8;                          // keys and requests of a tile
+  static constexpr int OROW = D * 4 + 16;                                 // bytes of an output row while the waves are joined
+  static constexpr int AREA = 32 * OROW > 16384 ? 32 * OROW : 16384;      // of a wave: K slot and V slot, then its output rows
+  static constexpr int STATS = NW * AREA, LDS_BYTES = STATS + NW * (32 * 8 + 4);
+  static __device__ __forceinline__ int kswz(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
+};
+
+// Lane L of a wave-wide request lands at lds + 16 L.
+__device__ __forceinline__ void request(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // until at most N requests are on their way
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+union Frag {
+  struct { s16x4 lo, hi; } s;
+  bf16x8 b;
+  u32x4 u;
+};
+// The larger magnitudes, half by half, as bit patterns: 0x7F80 and above are infinities and NaN.
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u16x2 larger_magnitude(u16x2 m, uint32_t x) {
+  return __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x & 0x7FFF7FFFu));
+}
+
+template <int D, bool PAGED, int NW>
+__device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item& it, int kvh) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  using C = FewCfg<D, NW>;
+  constexpr int ND = D / 16, NV = D / 32, NKB = C::BK / 32, NG = C::BK / 16, ROWB = C::ROWB, CPR = C::CPR, RPI = C::RPI;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int rw = lane & 31, h = lane >> 5;
+  const int group = a.hq / a.hkv, n_rows = it.q.n * group, r0 = it.tile * 32;
+  const int pos0 = it.q.len - it.q.n;  // slot of the first new token
+
+  const int r = min(r0 + rw, n_rows - 1), t = r / group, head = kvh * group + r % group;
+  const int t_first = r0 / group, t_last = min(r0 + 31, n_rows - 1) / group;
+  const int seen_first = pos0 + t_first + 1;                       // keys that the tile's first and last row see
+  const int begin = it.chunk * it.c, end = min(min(pos0 + t_last + 1, it.q.len), begin + it.c);
+  const int key_end = min(pos0 + t + 1, end);                      // one past the last key that counts for this lane's row
+
+  bf16x8 bq[ND];
+  {
+    const char* qp = a.q.p + head * a.q.hs + (long long)(it.q.first + t) * a.q.rs + h * 16;
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) bq[dc] = *reinterpret_cast<const bf16x8*>(qp + dc * 32);
+  }
+  const KvSource<PAGED> src{a, it.s, kvh, it.q.first, it.q.len - 1};
+  const uint32_t smem_at = (uint32_t)(size_t)(const __attribute__((address_space(3))) char*)smem;
+  const uint32_t k_lds = uniform(smem_at + wave * C::AREA), v_lds = k_lds + 8192;
+  const char* ks = smem + wave * C::AREA;
+  const char* vs = ks + 8192;
+
+  // Tiles are requested 16 keys at a time, which lie in one page.  Keys past the last one re-read that one: their weights are
+  // zero.
+  auto pages_of = [&](int k0, int (&pg)[NG]) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) pg[g] = src.page_of(k0 + 16 * g);
+  };
+  const int lrow = lane / CPR, pos = lane % CPR;
+  auto request_tile = [&](int k0, const int (&pg)[NG], const RowsArg& rows, bool is_v, uint32_t lds) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const char* base = rows.p + src.at(rows, min(k0 + 16 * g, src.last), pg[g]);
+      const int lim = max(src.last - k0 - 16 * g, 0);
+#pragma unroll
+      for (int i = 0; i < 16 / RPI; ++i) {
+        const int row = i * RPI + lrow;
+        const uint32_t chunk = (uint32_t)(pos ^ (is_v ? C::vswz(16 * g + row) : C::kswz(16 * g + row))) * 16;
+        request(base, (uint32_t)min(row, lim) * (uint32_t)rows.rs + chunk, lds + (g * (16 / RPI) + i) * 1024);
+      }
+    }
+  };
+
+  // LDS addresses of the fragments: every further one differs from the first in bits that the swizzle leaves to an exclusive or
+  uint32_t k_at = (uint32_t)(rw * ROWB + ((h ^ C::kswz(rw)) * 16)), v_at;
+  {
+    const int i16 = lane & 15, q2 = (lane >> 4) & 1, vrow = 4 * h + (i16 >> 2);
+    v_at = (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ C::vswz(vrow)) * 16) + 8 * (i16 & 1));
+  }
+
+  f32x16 o[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+  u16x2 most = {0, 0};  // magnitude of V
+  const float c2 = a.scale * kLog2e;
+
+  int k0 = begin + wave * C::BK;
+  int pg[NG];
+  if (k0 < end) {
+    pages_of(k0, pg);
+    request_tile(k0, pg, a.k, false, k_lds);
+    request_tile(k0, pg, a.v, true, v_lds);
+  }
+  for (; k0 < end; k0 += NW * C::BK) {
+    const int k1 = k0 + NW * C::BK;
+    const bool more = k1 < end;
+    if (more) pages_of(k1, pg);
+
+    wait_loads<C::NI>();  // K has landed, V may be on its way
+    bf16x8 ak[NKB][ND];
+    asm volatile("" : "+v"(k_at), "+v"(v_at));  // the exclusive ors stay in the loop, not in registers
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int dc = 0; dc < ND; ++dc) ak[kb][dc] = *reinterpret_cast<const bf16x8*>(ks + (k_at ^ (dc << 5)) + kb * 32 * ROWB);
+    wait_lds();
+    if (more) request_tile(k1, pg, a.k, false, k_lds);
+    f32x16 s[NKB];
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[kb][j] = 0.f;
+#pragma unroll
+      for (int dc = 0; dc < ND; ++dc) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[kb][dc], bq[dc], s[kb], 0, 0, 0);
+    }
+    // accumulator register j of block kb: key k0 + 32 kb + 8 (j / 4) + 4 h + j % 4
+    const bool masked = k0 + C::BK > min(seen_first, end);
+    const int n_ok = key_end - k0 - 4 * h;
+    if (masked) {
+#pragma unroll
+      for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (kb * 32 + 8 * (j >> 2) + (j & 3) >= n_ok) s[kb][j] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int kb = 0; kb < NKB; ++kb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[kb][j]);
+    mx = max_across_halves(mx);
+    const float m_new = fmaxf(m_run, mx * c2);
+    const float m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m_run - m_use);
+    m_run = m_new;
+    // Weights as the sum of two bf16 terms (16 significant bits): this kernel waits for memory, so the second product's
+    // second half costs nothing, and the outputs carry their own rounding alone.
+    bf16x8 bhi[NG], blo[NG];
+    float psum = 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + e], c2, -m_use));
+        psum += p;
+        bhi[g][e] = (__bf16)p;
+        blo[g][e] = (__bf16)(p - (float)bhi[g][e]);
+      }
+    l_run = fmaf(l_run, alpha, psum);
+    if (__any(alpha != 1.f)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] *= alpha;
+    }
+    if (more) wait_loads<C::NI>();
+    else wait_loads<0>();
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      Frag av[NV];
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb) {
+        const char* vp = vs + (v_at ^ (dvb << 6)) + g * 16 * ROWB;
+        av[dvb].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
+        av[dvb].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 8 * ROWB));
+      }
+      if (g == NG - 1) {
+        wait_lds();
+        if (more) request_tile(k1, pg, a.v, true, v_lds);
+      }
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) most = larger_magnitude(most, av[dvb].u[e]);
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb) {
+        o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[dvb].b, bhi[g], o[dvb], 0, 0, 0);
+        o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[dvb].b, blo[g], o[dvb], 0, 0, 0);
+      }
+    }
+  }
+
+  // join the waves: maxima and sums first, then the rows, each wave's scaled to the common maximum
+  float* s_m = reinterpret_cast<float*>(smem + C::STATS);
+  float* s_l = s_m + NW * 32;
+  int* s_bad = reinterpret_cast<int*>(s_l + NW * 32);
+  const bool bad = __any(most[0] >= 0x7F80 || most[1] >= 0x7F80);
+  const float l_row = sum_across_halves(l_run);
+  if (h == 0) {
+    s_m[wave * 32 + rw] = m_run;
+    s_l[wave * 32 + rw] = l_row;
+  }
+  if (lane == 0) s_bad[wave] = bad;
+  __syncthreads();
+  const int n_valid = min(32, n_rows - r0);
+  bool any_bad = false;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) any_bad |= s_bad[w] != 0;
+  if (any_bad) {
+    for (int row = wave; row < n_valid; row += NW) attend_row<true, D, PAGED>(a, it, src, r0 + row, begin, row);
+    return;
+  }
+  auto joined = [&](int row, float* m_out) {
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, s_m[w * 32 + row]);
+    const float m_use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l = fmaf(s_l[w * 32 + row], __builtin_amdgcn_exp2f(s_m[w * 32 + row] - m_use), l);
+    *m_out = m;
+    return l;
+  };
+  {
+    float m;
+    joined(rw, &m);
+    const float f = __builtin_amdgcn_exp2f(m_run - (m == -INFINITY ? 0.f : m));
+    char* mine = smem + wave * C::AREA + rw * C::OROW + h * 16;
+    if (rw < n_valid) {
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = o[dvb][4 * j4 + e] * f;
+          *reinterpret_cast<f32x4*>(mine + (dvb * 32 + 8 * j4) * 4) = x;
+        }
+    }
+  }
+  __syncthreads();
+  constexpr int LPR = D / 4;
+  for (int row = threadIdx.x / LPR; row < n_valid; row += NW * 64 / LPR) {
+    const int c4 = threadIdx.x % LPR;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(smem + w * C::AREA + row * C::OROW + c4 * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
+    float m;
+    const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= inv;
+    const float lse2 = m + __log2f(l);
+    if (it.n_chunks > 1) {
+      const long long at = ((long long)part_of(it, it.chunk) * a.hkv + kvh) * a.tile_rows + row;
+      *reinterpret_cast<f32x4*>(a.part_o + at * D + c4 * 4) = x;
+      if (c4 == 0) a.part_lse[at] = lse2;
+    } else {
+      const int rr = r0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+      const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+      *reinterpret_cast<bf16x4*>(a.out.p + hd * a.out.hs + tok * a.out.rs + c4 * 8) = y;
+      if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = lse2 * kLn2;
+    }
+  }
+}
+
+template <int D, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
+  const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
+  const Item it = find_item<32, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  if (it.s < 0) return;
+  attend_few<D, PAGED, 4>(a, it, kvh);
+}
+
+// out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
+// four channels a lane).
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
+  constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
+  const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
+  const int tile_no = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
+  const Item it = find_item<32, true>(a, group, tile_no, lane);
+  if (it.s < 0 || it.n_chunks == 1 || part_of(it, it.n_chunks - 1) >= a.max_items) return;
+  const int row = uniform(blockIdx.y * 4 + (threadIdx.x >> 6)), rr = it.tile * 32 + row;
+  if (row >= 32 || rr >= it.q.n * group) return;
+  const int c4 = lane % LPR, cg = lane / LPR;
+  auto at = [&](int c) { return ((long long)part_of(it, c) * a.hkv + kvh) * a.tile_rows + row; };
+  float m = -INFINITY, den = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int c0 = 0; c0 < it.n_chunks; c0 += 64) {
+    const float l = c0 + lane < it.n_chunks ? a.part_lse[at(c0 + lane)] : -INFINITY;
+    float mx = l;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
+    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = __builtin_amdgcn_exp2f(m - m_use), wt = __builtin_amdgcn_exp2f(l - m_use);
+    float sum = wt;
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
+    den = fmaf(den, alpha, sum);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+    m = m_new;
+    const int n = min(64, it.n_chunks - c0);
+    constexpr int U = 4;  // requests ahead
+    for (int c = 0; c < n; c += U * CG) {
+      f32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at(c0 + min(c + u * CG + cg, n - 1)) * D + c4 * 4);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int mine = c + u * CG + cg;
+        const float f = __shfl(wt, min(mine, 63));
+        if (mine < n) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, x[u][e], acc[e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int w = LPR; w < 64; w *= 2)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], w);
+  if (cg > 0) return;
+  const float inv = den == 0.f ? 0.f : 1.f / den;
+  const int tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+  char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
+  if constexpr (BF16) {
+    const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+    *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
+  } else {
+    *reinterpret_cast<f32x4*>(out + c4 * 16) = acc * inv;
+  }
+  if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------------------------- float32, and the host side
 template <bool BF16>
 __device__ __forceinline__ float element(const char* row, int c) {
   if constexpr (BF16) return (float)reinterpret_cast<const __bf16*>(row)[c];
@@ -68,21 +420,62 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttnLaunch a) {
   if (a.lse != nullptr && lane == 0) a.lse[(long long)head * a.b.n_rows + row] = m + logf(l);
 }
 
-template <bool BF16, int D>
-hipError_t run(const PagedAttnLaunch& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.b.n_rows + 3) / 4), (unsigned)a.hq);
-  if (a.paged) hipLaunchKernelGGL((k_paged_attn<BF16, D, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_paged_attn<BF16, D, false>), grid, dim3(256), 0, s, a);
+template <int D, bool PAGED>
+hipError_t run_few(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
+  hipLaunchKernelGGL((k_attend_few<D, PAGED>), dim3((unsigned)(p.max_items * a.hkv)), dim3(256), (FewCfg<D, 4>::LDS_BYTES), s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.joins) return e;
+  hipLaunchKernelGGL((k_join_chunks<D, true>), dim3((unsigned)(p.max_tiles * a.hkv), (unsigned)((p.tile_rows + 3) / 4)), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+template <int D>
+hipError_t run_f32(const PagedAttnLaunch& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.b.n_rows + 3) / 4), (unsigned)a.hq);
+  if (a.paged) hipLaunchKernelGGL((k_paged_attn<false, D, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_paged_attn<false, D, false>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int D, bool PAGED>
+hipError_t raise_limit() {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_few<D, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             FewCfg<D, 4>::LDS_BYTES);
 }
 
 }  // namespace
 
-size_t paged_attn_ws_bytes(int, int, int, int, int, int, int, int) { return 0; }
+PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool) {
+  PagedAttnPlan p;
+  const long long group = hq / hkv, tile = 32;
+  const long long by_bound = n_seq * ((max_new * group + tile - 1) / tile), by_rows = n_rows * group / tile + n_seq;
+  p.max_tiles = (int)(by_bound < by_rows ? by_bound : by_rows);
+  p.tile_rows = (int)(max_new * group < tile ? max_new * group : tile);
+  p.target = 512;     // as many workgroups as are resident at once
+  p.min_chunk = 256;
+  p.joins = dtype == SAMKV_BF16 && max_len > p.min_chunk;
+  p.max_items = p.max_tiles + (p.joins ? (p.target + hkv - 1) / hkv : 0);
+  if (!p.joins) p.min_chunk = max_len;
+  const size_t rows = p.joins ? (size_t)p.max_items * hkv * p.tile_rows : 0;
+  p.part_lse = (rows * d * 4 + 255) / 256 * 256;
+  p.bytes = p.part_lse + (rows * 4 + 255) / 256 * 256;
+  return p;
+}
+
+hipError_t paged_attn_raise_limits() {
+  const hipError_t all[] = {raise_limit<128, true>(), raise_limit<128, false>(), raise_limit<64, true>(), raise_limit<64, false>()};
+  for (hipError_t e : all)
+    if (e != hipSuccess) return e;
+  return hipSuccess;
+}
 
 hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s) {
-  if (a.dtype == SAMKV_BF16) return a.d == 128 ? run<true, 128>(a, s) : run<true, 64>(a, s);
-  return a.d == 128 ? run<false, 128>(a, s) : run<false, 64>(a, s);
+  if (a.dtype != SAMKV_BF16) return a.d == 128 ? run_f32<128>(a, s) : run_f32<64>(a, s);
+  const hipError_t e = attn_prepare_device();
+  if (e != hipSuccess) return e;
+  const PagedAttnPlan p = paged_attn_plan(a.dtype, a.d, a.hq, a.hkv, a.b.n_seq, a.b.n_rows, a.b.max_new, a.b.max_len, a.paged != 0);
+  if (a.paged) return a.d == 128 ? run_few<128, true>(a, p, s) : run_few<64, true>(a, p, s);
+  return a.d == 128 ? run_few<128, false>(a, p, s) : run_few<64, false>(a, p, s);
 }
 
 }  // namespace samkv

@@ -1028,13 +1028,24 @@ static int check_prompts(int n_seq, int n_tok, int max_len, int hq, int hkv, int
   return n_seq > SAMKV_MAX_SEQ || (long long)hq * n_tok > 0x7FFFFFFF / 256 ? SAMKV_EUNSUPPORTED : SAMKV_OK;
 }
 
+// Plan and workspace of an attention launch whose sizes are set.
+static int place_parts(PagedAttnLaunch* a, void* ws, size_t ws_bytes) {
+  const PagedAttnPlan p = paged_attn_plan(a->dtype, a->d, a->hq, a->hkv, a->b.n_seq, a->b.n_rows, a->b.max_new, a->b.max_len,
+                                          a->paged != 0);
+  if (!enough(ws, ws_bytes, p.bytes)) return SAMKV_EWORKSPACE;
+  a->target = p.target; a->min_chunk = p.min_chunk; a->max_items = p.max_items; a->tile_rows = p.tile_rows;
+  a->part_o = static_cast<float*>(ws);
+  a->part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + p.part_lse);
+  return SAMKV_OK;
+}
+
 static bool bad_lse(const float* lse) { return (uintptr_t)lse % 4 != 0; }
 
 size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t dtype) {
   if (check_prompts(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype) != SAMKV_OK) return 0;
   const int most = max_len < n_tok ? max_len : n_tok;
-  return paged_attn_ws_bytes(dtype, head_dim, n_q_heads, n_kv_heads, n_seq, n_tok, most, most);
+  return paged_attn_plan(dtype, head_dim, n_q_heads, n_kv_heads, n_seq, n_tok, most, most, false).bytes;
 }
 
 int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_rows* v, const int32_t* cu, int32_t n_seq,
@@ -1049,12 +1060,12 @@ int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_row
   if ((rc = check_rows(k, n_kv_heads, n_tok, head_dim, dtype, false, &a.k)) != SAMKV_OK) return rc;
   if ((rc = check_rows(v, n_kv_heads, n_tok, head_dim, dtype, false, &a.v)) != SAMKV_OK) return rc;
   if ((rc = check_rows(out, n_q_heads, n_tok, head_dim, dtype, true, &a.out)) != SAMKV_OK) return rc;
-  const size_t need = samkv_prefill_workspace_bytes(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype);
-  if (!enough(ws, ws_bytes, need)) return SAMKV_EWORKSPACE;
+  if (a.k.rs > (1 << 27) || a.v.rs > (1 << 27)) return SAMKV_EUNSUPPORTED;  // rows of a tile are told apart by 32-bit offsets
   a.dtype = dtype; a.d = head_dim; a.hq = n_q_heads; a.hkv = n_kv_heads; a.paged = 0;
   a.b.n_seq = n_seq; a.b.n_rows = n_tok; a.b.max_new = a.b.max_len = max_len < n_tok ? max_len : n_tok;
   a.b.cu = cu;
-  a.lse = lse; a.scale = scale; a.ws = ws;
+  a.lse = lse; a.scale = scale;
+  if ((rc = place_parts(&a, ws, ws_bytes)) != SAMKV_OK) return rc;
   return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -1087,7 +1098,8 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
 size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads) {
   BatchArg b;
   if (check_batch(pages, batch, n_q_heads, &b) != SAMKV_OK) return 0;
-  return paged_attn_ws_bytes(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new, b.max_len);
+  return paged_attn_plan(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new, b.max_len,
+                         true).bytes;
 }
 
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
@@ -1100,12 +1112,12 @@ int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const s
   const int d = pages->head_dim, dtype = pages->dtype, e = dtype == SAMKV_BF16 ? 2 : 4;
   if ((rc = check_rows(q, n_q_heads, batch->n_new, d, dtype, false, &a.q)) != SAMKV_OK) return rc;
   if ((rc = check_rows(out, n_q_heads, batch->n_new, d, dtype, true, &a.out)) != SAMKV_OK) return rc;
-  if (!enough(ws, ws_bytes, samkv_paged_workspace_bytes(pages, batch, n_q_heads))) return SAMKV_EWORKSPACE;
   a.dtype = dtype; a.d = d; a.hq = n_q_heads; a.hkv = pages->n_kv_heads; a.paged = 1;
   a.k.p = static_cast<char*>(pages->k); a.v.p = static_cast<char*>(pages->v);
   a.k.rs = a.v.rs = d * e;
   a.k.hs = a.v.hs = (long long)pages->page_size * d * e;
-  a.lse = lse; a.scale = scale; a.ws = ws;
+  a.lse = lse; a.scale = scale;
+  if ((rc = place_parts(&a, ws, ws_bytes)) != SAMKV_OK) return rc;
   return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -3,7 +3,7 @@ page numbers out of range in every test, and the workspace starts as garbage."""
 import numpy as np
 import pytest
 
-from tests.paged_cases import Paged
+from tests.paged_cases import Paged, check
 
 pytestmark = pytest.mark.gpu
 
@@ -94,11 +94,11 @@ def test_later_tokens_do_not_reach_a_row(dtype, d, hq, hkv, lens, new):
     for slot, (value, ch) in zip(slots, [(np.nan, 3), (np.inf, d - 1), (-np.inf, 0)]):
         x.v[x.table[s, slot // 16], :, slot % 16, ch] = value
     out, lse = x.attend(S)
+    # Rows that meet such values may be computed by other sums than before (each within the bound of check(), so the two runs
+    # are within twice that of each other): what is finite is held to the oracle, not to the bits of the clean run.
     ref = x.oracle()
-    assert np.array_equal(np.isnan(out), np.isnan(ref.out)) and np.array_equal(np.isinf(out), np.isinf(ref.out))
-    assert np.array_equal(out[np.isinf(out)], ref.out[np.isinf(out)])
-    fine = np.isfinite(ref.out)
-    assert np.array_equal(out[fine], clean[fine]) and np.array_equal(lse, clean_lse)
+    assert (~np.isfinite(ref.out)).any()
+    check(out, lse, ref, d, x.scale, dtype, "with infinities and NaN among the values")
     x = Paged(11 + d, dtype, d, hq, hkv, 16, lens, new)
     slot = lens[0] - n // 2
     x.k[x.table[s, slot // 16], :, slot % 16, 5] = np.nan

@@ -77,10 +77,11 @@ def test_later_rows_do_not_reach_a_row(dtype, d, hq, hkv, n):
     for at, value, ch in [(n - 2, np.nan, 3), (n // 2, np.inf, d - 1), (1, -np.inf, 0), (n + 49, np.nan, 1), (n + 50, np.inf, 2)]:
         v2[:, at, ch] = value
     out, lse = _run(dtype, q, k, v2, cu, n, scale)
-    ref = P.prefill(q, k, v2, cu, n, scale).out
-    assert np.array_equal(np.isnan(out), np.isnan(ref)) and np.array_equal(out[np.isinf(out)], ref[np.isinf(ref)])
-    fine = np.isfinite(ref)
-    assert np.array_equal(out[fine], clean[fine]) and np.array_equal(lse, clean_lse)
+    # Rows that meet such values may be computed by other sums than before (each within the bound of check(), so the two runs
+    # are within twice that of each other): what is finite is held to the oracle, not to the bits of the clean run.
+    ref = P.prefill(q, k, v2, cu, n, scale)
+    assert (~np.isfinite(ref.out)).any()
+    check(out, lse, ref, d, scale, dtype, "with infinities and NaN among the values")
     k2 = k.copy()
     k2[:, n // 2, 7] = np.nan
     out, lse = _run(dtype, q, k2, v, cu, n, scale)

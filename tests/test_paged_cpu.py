@@ -112,6 +112,9 @@ def test_refusals_of_paged_attention(S):  # noqa: F811
     for bad in (0.0, -1.0, math.inf, math.nan):
         assert call(scale=bad) == -1
     assert call(lse=FAKE + 2) == -1 and call(hq=7) == -1 and call(hq=0) == -1
+    long = dict(max_pages=1000, max_len=16000)
+    assert S._lib.samkv_paged_workspace_bytes(_pages(S), _batch(S, **long), 8) > 1024
+    assert call(batch=long, ws=None) == -3 and call(batch=long, n=16) == -3 and call(batch=long, ws=FAKE * 256 + 16) == -3
 
 
 def test_refusals_of_prefill(S):  # noqa: F811
@@ -129,7 +132,7 @@ def test_refusals_of_prefill(S):  # noqa: F811
     for kw, code in [(dict(cu=None), -1), (dict(cu=FAKE + 2), -1), (dict(n_seq=0), -1), (dict(n=0), -1), (dict(max_len=0), -1),
                      (dict(hq=7), -1), (dict(hq=0), -1), (dict(hkv=0), -1), (dict(d=80), -2), (dict(dtype=5), -2),
                      (dict(scale=0.0), -1), (dict(scale=math.nan), -1), (dict(lse=FAKE + 1), -1), (dict(n_seq=5000), -2),
-                     (dict(n=1 << 24), -2)]:
+                     (dict(n=1 << 24), -2), (dict(k=dict(rs=1 << 27)), -2), (dict(v=dict(rs=1 << 27)), -2)]:
         assert call(**kw) == code, kw
     assert S._lib.samkv_prefill_workspace_bytes(0, 6, 4, 8, 2, 128, 1) == 0
 
