@@ -72,17 +72,19 @@ struct PagedAttnLaunch {
   RowsArg k, v;  // pages: hs = bytes of one head's rows of a page, rs = bytes of a row
   float* lse;    // may be null
   float scale;
-  int target, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys
-  int max_items;          // items there is room for
-  int tile_rows;          // rows of a tile that partial results have room for
-  float* part_o;          // [max_items][hkv][tile_rows][d], normalised
-  float* part_lse;        // [max_items][hkv][tile_rows], in units of log 2
+  int target, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys (wide tiles: twice that)
+  int max_chunks;         // 1: no sequence's keys are cut
+  // partial results of the tiles whose keys are cut, in slots of 32 rows (of tile_rows, where no tile has more)
+  int max_slots, tile_rows;
+  float* part_o;          // [max_slots][hkv][tile_rows][d], normalised
+  float* part_lse;        // [max_slots][hkv][tile_rows], in units of log 2
 };
 hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
 
 // Sizes of a launch that follow from the bounds alone.
 struct PagedAttnPlan {
-  int target, min_chunk, max_tiles, max_items, tile_rows;
+  bool wide;   // whether any sequence can have more than kFewRows rows per KV head and a kernel for them
+  int target, min_chunk, max_items, max_slots, tile_rows;
   bool joins;  // whether any sequence can have more than one chunk
   size_t part_lse, bytes;  // workspace: part_o, then part_lse
 };

@@ -275,7 +275,7 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
     for (int e = 0; e < 4; ++e) x[e] *= inv;
     const float lse2 = m + __log2f(l);
     if (it.n_chunks > 1) {
-      const long long at = ((long long)part_of(it, it.chunk) * a.hkv + kvh) * a.tile_rows + row;
+      const long long at = part_row(a, it, it.chunk, kvh) + row;
       *reinterpret_cast<f32x4*>(a.part_o + at * D + c4 * 4) = x;
       if (c4 == 0) a.part_lse[at] = lse2;
     } else {
@@ -290,24 +290,350 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
 template <int D, bool PAGED>
 __global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
   const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<32, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
-  if (it.s < 0) return;
+  const Item it = find_item<false, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  if (it.s < 0 || !has_room(a, it)) return;
   attend_few<D, PAGED, 4>(a, it, kvh);
+}
+
+// ---------------------------------------------------------------------------------------------- many rows
+// Eight waves of 32 rows each, one workgroup per compute unit; tiles of 64 keys that all waves read.  K and V tiles travel
+// straight into a ring of three LDS slots each, requested two steps ahead of their use.  Inside a wave the products of the next
+// tile's scores are issued in one block with the weights of the current one, so that the matrix unit and the vector unit work at
+// the same time:
+//     step t:  S(t+1) = K(t+1) Q^T (matrix)  |  P(t) = 2^(S(t) c - m) (vector);  O^T += V(t)^T P(t)^T (matrix)
+// The running maximum is raised only when a row outgrows it by 2^8, which keeps the rescaling of O off the common path: weights
+// stay below 256.  They are rounded to bf16 (half a step, 2^-8 relative, as the output is in the end); their sum is that of the
+// unrounded weights, in float32.
+template <int D>
+struct WideCfg {
+  static constexpr int NW = 8, BK = 64, NSLOT = 3;
+  static constexpr int ROWB = D * 2, CPR = ROWB / 16, RPI = 1024 / ROWB;
+  static constexpr int TILE = BK * ROWB, NI = TILE / 1024 / NW;  // a wave requests 8 rows of a tile, which lie in one page
+  static constexpr int LDS_BYTES = 2 * NSLOT * TILE;
+  static_assert(NI * RPI == 8, "rows of a wave");
+};
+
+template <int D, bool PAGED>
+__device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item& it, int kvh) {
+  using C = WideCfg<D>;
+  using F = FewCfg<D, 8>;  // the swizzles
+  constexpr int ND = D / 16, NV = D / 32, ROWB = C::ROWB, CPR = C::CPR, NI = C::NI, TILE = C::TILE, BK = C::BK;
+  constexpr float TAU = 8.f;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  // K(j) in slot j % 3 at smem + slot * TILE, V(j) at smem + (3 + slot) * TILE
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int rw = lane & 31, h = lane >> 5;
+  const int group = a.hq / a.hkv, n_rows = it.q.n * group, r0 = it.tile * kWideRows + wave * 32;
+  const int pos0 = it.q.len - it.q.n;
+  auto slots_seen = [&](int r) { return min(pos0 + min(r, n_rows - 1) / group + 1, it.q.len); };  // keys that row r sees
+
+  const int begin = it.chunk * it.c;
+  const int end = min(slots_seen(it.tile * kWideRows + kWideRows - 1), begin + it.c);
+  const int n_tiles = max((end - begin + BK - 1) / BK, 0);
+  const bool has_rows = r0 < n_rows;
+  const int seen_first = has_rows ? min(slots_seen(r0), end) : begin, seen_last = has_rows ? min(slots_seen(r0 + 31), end) : begin;
+  const int n_full = max(seen_first - begin, 0) / BK, n_any = max(seen_last - begin + BK - 1, 0) / BK;  // unmasked tiles; tiles
+
+  const int r = min(r0 + rw, n_rows - 1);
+  const int key_end = min(slots_seen(r), end);
+  bf16x8 bq[ND];
+  {
+    const char* qp = a.q.p + (kvh * group + r % group) * a.q.hs + (long long)(it.q.first + r / group) * a.q.rs + h * 16;
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) bq[dc] = *reinterpret_cast<const bf16x8*>(qp + dc * 32);
+  }
+
+  // ---- requests: rows 8 wave .. 8 wave + 7 of every tile.  The pages of 64 tiles are looked up at once, one per lane.
+  const KvSource<PAGED> src{a, it.s, kvh, it.q.first, it.q.len - 1};
+  const uint32_t smem_at = (uint32_t)(size_t)(const __attribute__((address_space(3))) char*)smem;
+  const uint32_t wave_rows = uniform(smem_at + NI * wave * 1024);
+  const int key0 = begin + 8 * wave;
+  int pages = 0;
+  auto look_up = [&](int j) {
+    if constexpr (PAGED) {
+      const int key = min(key0 + (j + lane) * BK, src.last);
+      pages = min(max(a.b.table[(long long)it.s * a.b.max_pages + (key >> a.b.page_log2)], 0), a.b.n_pages - 1);
+    }
+  };
+  auto page_of = [&](int j) { return PAGED ? __builtin_amdgcn_readlane(pages, j & 63) : 0; };
+  auto request_rows = [&](const RowsArg& rows, bool is_v, int j, int page, uint32_t slot) {
+    const int key = key0 + j * BK;
+    const char* base = rows.p + src.at(rows, min(key, src.last), page);
+    const int lim = max(src.last - key, 0);
+    int l = lane;
+    asm volatile("" : "+v"(l));  // offsets are made here, not kept in registers
+    const int lrow = l / CPR, pos = l % CPR;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int row = i * C::RPI + lrow;
+      const uint32_t chunk = (uint32_t)(pos ^ (is_v ? F::vswz(row) : F::kswz(8 * wave + row))) * 16;
+      request(base, (uint32_t)min(row, lim) * (uint32_t)rows.rs + chunk, wave_rows + slot + i * 1024);
+    }
+  };
+  auto k_off = [&](int j) { return (uint32_t)((j % 3) * TILE); };
+  auto v_off = [&](int j) { return (uint32_t)((3 + j % 3) * TILE); };
+  auto request_k = [&](int j, int page) { request_rows(a.k, false, j, page, k_off(j)); };
+  auto request_v = [&](int j, int page) { request_rows(a.v, true, j, page, v_off(j)); };
+
+  // ---- fragments: LDS addresses of the first one in slot 0; the others differ in bits that an exclusive or turns (slots are
+  // multiples of 1 KB).  Made where they are used: kept, they would cost registers that the two sets of scores need.
+  const uint32_t k_at = (uint32_t)(rw * ROWB + ((h ^ F::kswz(rw)) * 16));
+  uint32_t v_at;
+  {
+    const int i16 = lane & 15, q2 = (lane >> 4) & 1, vrow = 4 * h + (i16 >> 2);
+    v_at = (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ F::vswz(vrow)) * 16) + 8 * (i16 & 1));
+  }
+  auto kfrags = [&](uint32_t slot, int kb, bf16x8 (&ak)[ND]) {
+    uint32_t at = k_at + slot;
+    asm volatile("" : "+v"(at));
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) ak[dc] = *reinterpret_cast<const bf16x8*>(smem + (at ^ (dc << 5)) + kb * 32 * ROWB);
+  };
+  auto vfrags = [&](uint32_t at, int g, Frag (&av)[NV]) {
+#pragma unroll
+    for (int dvb = 0; dvb < NV; ++dvb) {
+      const char* vp = smem + (at ^ (dvb << 6)) + g * 16 * ROWB;
+      av[dvb].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
+      av[dvb].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 8 * ROWB));
+    }
+  };
+
+  f32x16 o[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
+  float m_ref = -INFINITY, l_run = 0.f;
+  u16x2 most = {0, 0};  // magnitude of V in masked tiles
+  const float c2 = a.scale * kLog2e;
+
+  auto lift = [&](float mx) {
+    if (__any(mx > m_ref + TAU)) {
+      const float m_new = fmaxf(m_ref, mx);
+      const float al = __builtin_amdgcn_exp2f(m_ref - (m_new == -INFINITY ? 0.f : m_new));
+      l_run *= al;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[i][j] *= al;
+      m_ref = m_new;
+    }
+  };
+  auto row_max = [&](const f32x16 (&s)[2]) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[kb][j]);
+    return max_across_halves(mx) * c2;
+  };
+  // LDS reads may not be moved across this point (everything else may): a fragment load stays one group of products ahead of
+  // its use
+  constexpr int kHoldLds = 0x47F;
+  auto weights_pv = [&](f32x16 (&s)[2], uint32_t slot, bool masked) {
+    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+    uint32_t vs = v_at + slot;
+    asm volatile("" : "+v"(vs));
+    bf16x8 bp[4];
+    Frag va[2][NV];
+    vfrags(vs, 0, va[0]);  // lands while the weights are computed
+    __builtin_amdgcn_sched_barrier(kHoldLds);
+    float psum = 0.f;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + e], c2, -m_use));
+        psum += p;
+        bp[g][e] = (__bf16)p;
+      }
+    l_run += psum;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (g + 1 < 4) {
+        vfrags(vs, g + 1, va[(g + 1) & 1]);
+        __builtin_amdgcn_sched_barrier(kHoldLds);
+      }
+      if (masked) {
+#pragma unroll
+        for (int dvb = 0; dvb < NV; ++dvb)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most = larger_magnitude(most, va[g & 1][dvb].u[e]);
+      }
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb)
+        o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[g & 1][dvb].b, bp[g], o[dvb], 0, 0, 0);
+    }
+  };
+  auto mask = [&](int tile, f32x16 (&s)[2]) {
+    int n_ok = key_end - begin - tile * BK - 4 * h;  // keys of the tile that count, less the lane's first: made here
+    asm volatile("" : "+v"(n_ok));
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int j = 0; j < 16; ++j)
+        if (kb * 32 + 8 * (j >> 2) + (j & 3) >= n_ok) s[kb][j] = -INFINITY;
+  };
+  auto scores = [&](uint32_t ks, f32x16 (&s)[2]) {
+    bf16x8 ak0[ND], ak1[ND];
+    kfrags(ks, 0, ak0);
+    kfrags(ks, 1, ak1);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) { s[0][j] = 0.f; s[1][j] = 0.f; }
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak0[dc], bq[dc], s[0], 0, 0, 0);
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak1[dc], bq[dc], s[1], 0, 0, 0);
+  };
+
+  if (n_tiles > 0) {
+    look_up(0);
+    int page_v = 0, page_k = page_of(0);
+    request_k(0, page_k);
+    request_v(0, page_k);
+    if (n_tiles > 1) {
+      page_k = page_of(1);
+      request_k(1, page_k);
+      request_v(1, page_k);
+    }
+    if (n_tiles > 2) {
+      page_k = page_of(2);
+      request_k(2, page_k);
+    }
+    // K(0) for the first scores
+    if (n_tiles > 2) wait_loads<4 * NI>();
+    else if (n_tiles > 1) wait_loads<3 * NI>();
+    else wait_loads<NI>();
+    __builtin_amdgcn_s_barrier();
+    f32x16 sA[2], sB[2];
+    scores(0, sA);
+    // V(0) and K(1) for step 0; K(0) has been read by every wave before step 0 requests its slot's next tile
+    if (n_tiles > 2) wait_loads<2 * NI>();
+    else if (n_tiles > 1) wait_loads<NI>();
+    else wait_loads<0>();
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+
+    // Every wave walks all tiles: it requests its rows and meets the barriers, whatever it computes.
+    auto ahead = [&](int tile) {
+      page_v = page_k;
+      if (tile + 3 < n_tiles) {
+        if (PAGED && ((tile + 3) & 63) == 0) look_up(tile + 3);
+        page_k = page_of(tile + 3);
+        request_k(tile + 3, page_k);
+      }
+      if (tile + 2 < n_tiles) request_v(tile + 2, page_v);
+    };
+    auto done = [&](int tile) {  // the next step's tiles were requested one step ago: all but this step's requests have to land
+      if (tile + 3 < n_tiles) wait_loads<2 * NI>();
+      else if (tile + 2 < n_tiles) wait_loads<NI>();
+      else wait_loads<0>();
+      wait_lds();
+      __builtin_amdgcn_s_barrier();
+    };
+    // unmasked tiles, two at a time: S(tile) is in sc, S(tile + 1) goes to sn
+    auto step = [&](int tile, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+      ahead(tile);
+      const uint32_t k_next = k_off(tile + 1);
+      bf16x8 ak0[ND], ak1[ND];
+      kfrags(k_next, 0, ak0);
+      lift(row_max(sc));
+      kfrags(k_next, 1, ak1);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) { sn[0][j] = 0.f; sn[1][j] = 0.f; }
+#pragma unroll
+      for (int dc = 0; dc < ND; ++dc) sn[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak0[dc], bq[dc], sn[0], 0, 0, 0);
+#pragma unroll
+      for (int dc = 0; dc < ND; ++dc) sn[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak1[dc], bq[dc], sn[1], 0, 0, 0);
+      weights_pv(sc, v_off(tile), false);
+      done(tile);
+    };
+    int tile = 0;
+    for (; tile + 1 < n_full; tile += 2) {
+      step(tile, sA, sB);
+      step(tile + 1, sB, sA);
+    }
+    // the masked ones behind them, and an odd unmasked one
+    for (; tile < n_any; ++tile) {
+      ahead(tile);
+      mask(tile, sA);
+      lift(row_max(sA));
+      weights_pv(sA, v_off(tile), true);
+      if (tile + 1 < n_any) scores(k_off(tile + 1), sA);
+      done(tile);
+    }
+    for (; tile < n_tiles; ++tile) {
+      ahead(tile);
+      done(tile);
+    }
+  }
+
+  if (!has_rows) return;
+  int rw_end = lane & 31;
+  asm volatile("" : "+v"(rw_end));  // the row again: kept, it would cost registers
+  const int n_valid = min(32, n_rows - r0);
+  if (__any(most[0] >= 0x7F80 || most[1] >= 0x7F80)) {
+    for (int row = 0; row < n_valid; ++row) attend_row<true, D, PAGED>(a, it, src, r0 + row, begin, wave * 32 + row);
+    return;
+  }
+  const float l_tot = sum_across_halves(l_run), inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+  const float lse2 = m_ref + __log2f(l_tot);
+  char* turn = smem + wave * (C::LDS_BYTES / 8);  // of this wave alone: the ring is free since the last barrier
+  if (it.n_chunks > 1) {
+    const long long at = part_row(a, it, it.chunk, kvh) + wave * 32;
+    store_rows_via_lds<D, 2>(o, inv, a.part_o + at * D, n_valid, turn, lane);
+    if (h == 0 && rw < n_valid) a.part_lse[at + rw] = lse2;
+    return;
+  }
+  constexpr int RS = ROWB + 16;
+  static_assert(32 * RS <= C::LDS_BYTES / 8 && 16 * (D * 4 + 16) <= C::LDS_BYTES / 8, "rows are turned in the ring");
+#pragma unroll
+  for (int dvb = 0; dvb < NV; ++dvb)
+#pragma unroll
+    for (int j4 = 0; j4 < 4; ++j4) {
+      const bf16x4 y = {(__bf16)(o[dvb][4 * j4] * inv), (__bf16)(o[dvb][4 * j4 + 1] * inv), (__bf16)(o[dvb][4 * j4 + 2] * inv),
+                        (__bf16)(o[dvb][4 * j4 + 3] * inv)};
+      *reinterpret_cast<bf16x4*>(turn + rw * RS + (dvb * 32 + 8 * j4 + 4 * h) * 2) = y;
+    }
+  const int r_end = min(r0 + rw_end, n_rows - 1);
+  const int head = kvh * group + r_end % group, tok = it.q.first + r_end / group, lrow = lane / CPR, pos = lane % CPR;
+  const long long to = head * a.out.hs + tok * a.out.rs;
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < 32 / C::RPI; ++i) {
+    const int row = i * C::RPI + lrow;
+    const u32x4 y = *reinterpret_cast<const u32x4*>(turn + row * RS + pos * 16);
+    const uint32_t lo = __shfl((uint32_t)to, row), hi = __shfl((uint32_t)((unsigned long long)to >> 32), row);
+    if (row < n_valid) *reinterpret_cast<u32x4*>(a.out.p + (long long)((unsigned long long)hi << 32 | lo) + pos * 16) = y;
+  }
+  if (h == 0 && rw < n_valid && a.lse != nullptr) a.lse[(long long)head * a.b.n_rows + tok] = lse2 * kLn2;
+}
+
+// Batches in which some sequences have many rows: 256 at a time for those, 32 shared by the eight waves for the others.
+template <int D, bool PAGED>
+__global__ __launch_bounds__(512, 2) void k_attend_mixed(PagedAttnLaunch a) {
+  const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
+  const Item it = find_item<true, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  if (it.s < 0 || !has_room(a, it)) return;
+  if (it.wide) attend_wide<D, PAGED>(a, it, kvh);
+  else attend_few<D, PAGED, 8>(a, it, kvh);
 }
 
 // out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
 // four channels a lane).
-template <int D, bool BF16>
+template <int D, bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
   constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
   const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
-  const int tile_no = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<32, true>(a, group, tile_no, lane);
-  if (it.s < 0 || it.n_chunks == 1 || part_of(it, it.n_chunks - 1) >= a.max_items) return;
-  const int row = uniform(blockIdx.y * 4 + (threadIdx.x >> 6)), rr = it.tile * 32 + row;
-  if (row >= 32 || rr >= it.q.n * group) return;
+  const int kvh = blockIdx.x % a.hkv;
+  int rows32 = 0;
+  const Item it = find_item<WIDE, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
+  if (it.s < 0 || !has_room(a, it)) return;
+  const int tile0 = it.tile * 32 * it.slots(), n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
+  for (int row = rows32 * 32 + uniform(blockIdx.y * 4 + (threadIdx.x >> 6)); row < n_rows; row += 4 * gridDim.y) {
+  const int rr = tile0 + row;
   const int c4 = lane % LPR, cg = lane / LPR;
-  auto at = [&](int c) { return ((long long)part_of(it, c) * a.hkv + kvh) * a.tile_rows + row; };
+  auto at = [&](int c) { return part_row(a, it, c, kvh) + row; };
   float m = -INFINITY, den = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   for (int c0 = 0; c0 < it.n_chunks; c0 += 64) {
@@ -346,7 +672,7 @@ __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
   for (int w = LPR; w < 64; w *= 2)
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], w);
-  if (cg > 0) return;
+  if (cg > 0) continue;
   const float inv = den == 0.f ? 0.f : 1.f / den;
   const int tok = it.q.first + rr / group, hd = kvh * group + rr % group;
   char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
@@ -357,6 +683,7 @@ __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
     *reinterpret_cast<f32x4*>(out + c4 * 16) = acc * inv;
   }
   if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- float32, and the host side
@@ -420,12 +747,21 @@ __global__ __launch_bounds__(256) void k_paged_attn(PagedAttnLaunch a) {
   if (a.lse != nullptr && lane == 0) a.lse[(long long)head * a.b.n_rows + row] = m + logf(l);
 }
 
+template <int D>
+constexpr int mixed_lds() {
+  return WideCfg<D>::LDS_BYTES > FewCfg<D, 8>::LDS_BYTES ? WideCfg<D>::LDS_BYTES : FewCfg<D, 8>::LDS_BYTES;
+}
+
 template <int D, bool PAGED>
-hipError_t run_few(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
-  hipLaunchKernelGGL((k_attend_few<D, PAGED>), dim3((unsigned)(p.max_items * a.hkv)), dim3(256), (FewCfg<D, 4>::LDS_BYTES), s, a);
+hipError_t run_bf16(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)(p.max_items * a.hkv));
+  if (p.wide) hipLaunchKernelGGL((k_attend_mixed<D, PAGED>), grid, dim3(512), mixed_lds<D>(), s, a);
+  else hipLaunchKernelGGL((k_attend_few<D, PAGED>), grid, dim3(256), (FewCfg<D, 4>::LDS_BYTES), s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.joins) return e;
-  hipLaunchKernelGGL((k_join_chunks<D, true>), dim3((unsigned)(p.max_tiles * a.hkv), (unsigned)((p.tile_rows + 3) / 4)), dim3(256), 0, s, a);
+  const dim3 join((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.wide ? 1 : (p.tile_rows + 3) / 4));
+  if (p.wide) hipLaunchKernelGGL((k_join_chunks<D, true, true>), join, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_join_chunks<D, true, false>), join, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -439,26 +775,34 @@ hipError_t run_f32(const PagedAttnLaunch& a, hipStream_t s) {
 
 template <int D, bool PAGED>
 hipError_t raise_limit() {
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_few<D, PAGED>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             FewCfg<D, 4>::LDS_BYTES);
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_few<D, PAGED>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 4>::LDS_BYTES);
+  return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_mixed<D, PAGED>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, mixed_lds<D>());
 }
 
 }  // namespace
 
-PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool) {
+PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
-  const long long group = hq / hkv, tile = 32;
-  const long long by_bound = n_seq * ((max_new * group + tile - 1) / tile), by_rows = n_rows * group / tile + n_seq;
-  p.max_tiles = (int)(by_bound < by_rows ? by_bound : by_rows);
-  p.tile_rows = (int)(max_new * group < tile ? max_new * group : tile);
-  p.target = 512;     // as many workgroups as are resident at once
+  const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
+  auto less = [](long long x, long long y) { return x < y ? x : y; };
+  p.wide = dtype == SAMKV_BF16 && most > kFewRows;
+  p.target = p.wide ? 256 : 512;  // as many workgroups as are resident at once
   p.min_chunk = 256;
-  p.joins = dtype == SAMKV_BF16 && max_len > p.min_chunk;
-  p.max_items = p.max_tiles + (p.joins ? (p.target + hkv - 1) / hkv : 0);
-  if (!p.joins) p.min_chunk = max_len;
-  const size_t rows = p.joins ? (size_t)p.max_items * hkv * p.tile_rows : 0;
-  p.part_lse = (rows * d * 4 + 255) / 256 * 256;
-  p.bytes = p.part_lse + (rows * 4 + 255) / 256 * 256;
+  // Prompts that fill the chip many times over are not cut: the join would be one more launch.
+  p.joins = dtype == SAMKV_BF16 && max_len > p.min_chunk && (paged || rows / kWideRows * hkv < 4 * p.target);
+  // Items: the tiles of 32 rows that there can be, or of 256 and those of sequences with few rows, and the chunks that find_item
+  // cuts (a chunk holds at least 1 / target of the cost of all heads, and a tile's cost is at least half of its keys').
+  const long long few_most = p.wide ? kFewRows : most, per = p.wide ? kWideRows / 32 : 1, shares = (p.target + hkv - 1) / hkv;
+  const long long tiles = less(n * ((few_most + 31) / 32), rows / 32 + n) + (p.wide ? less(n * ((most + kWideRows - 1) / kWideRows), rows / kWideRows + n) : 0);
+  p.max_items = (int)(tiles + (p.joins ? 2 * shares : 0));
+  // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
+  p.max_slots = (int)(p.joins ? less(p.max_items, 4 * shares) * per : 0);
+  p.tile_rows = (int)less(32, most);
+  const size_t part_rows = (size_t)p.max_slots * hkv * p.tile_rows;
+  p.part_lse = (part_rows * d * 4 + 255) / 256 * 256;
+  p.bytes = p.part_lse + (part_rows * 4 + 255) / 256 * 256;
   return p;
 }
 
@@ -474,8 +818,8 @@ hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s) {
   const hipError_t e = attn_prepare_device();
   if (e != hipSuccess) return e;
   const PagedAttnPlan p = paged_attn_plan(a.dtype, a.d, a.hq, a.hkv, a.b.n_seq, a.b.n_rows, a.b.max_new, a.b.max_len, a.paged != 0);
-  if (a.paged) return a.d == 128 ? run_few<128, true>(a, p, s) : run_few<64, true>(a, p, s);
-  return a.d == 128 ? run_few<128, false>(a, p, s) : run_few<64, false>(a, p, s);
+  if (a.paged) return a.d == 128 ? run_bf16<128, true>(a, p, s) : run_bf16<64, true>(a, p, s);
+  return a.d == 128 ? run_bf16<128, false>(a, p, s) : run_bf16<64, false>(a, p, s);
 }
 
 }  // namespace samkv

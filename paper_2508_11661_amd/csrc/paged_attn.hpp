@@ -20,49 +20,67 @@ __device__ __forceinline__ int scan64(int x, int lane) {  // inclusive prefix su
   return x;
 }
 
+// Sequences of at most kFewRows rows per KV head are cut into tiles of 32 rows, the others, where there is a kernel for that
+// (WIDE), into tiles of kWideRows.
+constexpr int kFewRows = 128, kWideRows = 256;
+constexpr int kWideCost = 5;  // time of a wide tile over a number of keys, in tiles of 32 rows
+
 struct Item {
   int s;                     // sequence; < 0: no item
+  bool wide;
   int tile, chunk, n_chunks, tiles;
   int c;                     // keys of a chunk
-  int first_part;            // items ahead of the sequence's
+  int first_slot;            // slots of partial results ahead of the sequence's
   SeqSpan q;
+  __device__ __forceinline__ int slots() const { return wide ? kWideRows / 32 : 1; }  // of a (tile, chunk) that is a part
 };
 
-// Item number `index`, or, with BY_TILE, the sequence and tile of row tile number `index` (chunk 0).  Called by whole waves; the
-// result is the same in every lane.  Within a sequence items run chunk by chunk, the last tile (with the most keys) first.
-template <int TILE_ROWS, bool BY_TILE>
-__device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, int index, int lane) {
+// Item number `index`.  JOIN: group of 32 rows number `index` among the tiles whose keys are cut; *rows32 is the group's number in
+// its tile, and the chunk is the first.  Called by whole waves; the result is the same in every lane.  Within a sequence items
+// run chunk by chunk, the last tile (with the most keys) first.
+template <bool WIDE, bool JOIN>
+__device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, int index, int lane, int* rows32 = nullptr) {
   const BatchArg& b = a.b;
   auto span = [&](int s) {
     SeqSpan q = seq_span(b, min(s, b.n_seq - 1));
     if (s >= b.n_seq) q.n = q.len = 0;
     return q;
   };
-  auto n_tiles = [&](const SeqSpan& q) { return (int)(((long long)q.n * group + TILE_ROWS - 1) / TILE_ROWS); };
+  auto is_wide = [&](const SeqSpan& q) { return WIDE && (long long)q.n * group > kFewRows; };
+  auto n_tiles = [&](const SeqSpan& q) {
+    const int rows = is_wide(q) ? kWideRows : 32;
+    return (int)(((long long)q.n * group + rows - 1) / rows);
+  };
   SeqSpan q = span(lane);
   int tiles = n_tiles(q);
-  // keys of a chunk: those of all tiles and heads over the number of workgroups
-  unsigned long long total = 0;
-  for (int s = lane; s < b.n_seq; s += 64) {
-    const SeqSpan x = s == lane ? q : span(s);
-    total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * x.len;
-  }
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w);
-  const unsigned long long share = (total * a.hkv + a.target - 1) / a.target;
   Item it;
-  it.c = uniform((int)min((share + 63) / 64 * 64, 0x40000000ull));
-  it.c = max(it.c, a.min_chunk);
+  it.c = 0x40000000;
+  if (a.max_chunks > 1) {
+    // keys of a chunk of 32 rows: the cost of all tiles and heads over the number of workgroups; a wide tile's are fewer by
+    // what it costs more.  A tile of new tokens sees on average half of them, and at least half of len.
+    unsigned long long total = 0;
+    for (int s = lane; s < b.n_seq; s += 64) {
+      const SeqSpan x = s == lane ? q : span(s);
+      const long long keys = max(x.len - x.n / 2, (x.len + 1) / 2);
+      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * keys * (is_wide(x) ? kWideCost : 1);
+    }
+#pragma unroll
+    for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w);
+    const unsigned long long share = (total * a.hkv + a.target - 1) / a.target;
+    it.c = uniform((int)min(share, 0x40000000ull));
+  }
+  const int c_few = max((it.c + 63) / 64 * 64, a.min_chunk), c_wide = max((it.c / kWideCost + 64) / 64 * 64, 2 * a.min_chunk);
   it.s = -1;
-  int tiles_before = 0, items_before = 0;
+  int before = 0, slots_before = 0;
   for (int s0 = 0; s0 < b.n_seq; s0 += 64) {
     if (s0 > 0) {
       q = span(s0 + lane);
       tiles = n_tiles(q);
     }
-    const int chunks = max((q.len + it.c - 1) / it.c, 1), items = tiles * chunks;
-    const int tiles_to = scan64(tiles, lane) + tiles_before, items_to = scan64(items, lane) + items_before;
-    const int upto = BY_TILE ? tiles_to : items_to;
+    const int c = is_wide(q) ? c_wide : c_few, per = is_wide(q) ? kWideRows / 32 : 1;
+    const int chunks = max((q.len + c - 1) / c, 1), items = tiles * chunks, slots = chunks > 1 ? items * per : 0;
+    const int count = JOIN ? (chunks > 1 ? tiles * per : 0) : items;
+    const int upto = scan64(count, lane) + before, slots_to = scan64(slots, lane) + slots_before;
     const unsigned long long past = __ballot(upto > index);
     if (past != 0) {
       const int at = __ffsll(past) - 1;
@@ -70,23 +88,41 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
       it.s = s0 + at;
       it.tiles = of(tiles);
       it.n_chunks = of(chunks);
-      it.first_part = of(items_to - items);
+      it.first_slot = of(slots_to - slots);
       it.q.first = of(q.first);
       it.q.n = of(q.n);
       it.q.len = of(q.len);
-      const int local = index - (BY_TILE ? of(tiles_to - tiles) : it.first_part);
-      it.chunk = BY_TILE ? 0 : local / it.tiles;
-      it.tile = it.tiles - 1 - (BY_TILE ? local : local % it.tiles);
+      it.wide = is_wide(it.q);
+      it.c = it.wide ? c_wide : c_few;
+      const int local = index - of(upto - count);
+      if constexpr (JOIN) {
+        it.chunk = 0;
+        it.tile = local / it.slots();
+        *rows32 = local % it.slots();
+      } else {
+        it.chunk = local / it.tiles;
+        it.tile = it.tiles - 1 - local % it.tiles;
+      }
       return it;
     }
-    tiles_before = uniform(__shfl(tiles_to, 63));
-    items_before = uniform(__shfl(items_to, 63));
+    before = uniform(__shfl(upto, 63));
+    slots_before = uniform(__shfl(slots_to, 63));
   }
   return it;
 }
 
-// Number of a (tile, chunk)'s partial result.
-__device__ __forceinline__ int part_of(const Item& it, int chunk) { return it.first_part + chunk * it.tiles + it.tiles - 1 - it.tile; }
+// First slot of a (tile, chunk)'s partial result (one of every KV head stands there), and the row of part_lse and part_o that
+// one head's begins at.
+__device__ __forceinline__ int part_slot(const Item& it, int chunk) {
+  return it.first_slot + (chunk * it.tiles + it.tiles - 1 - it.tile) * it.slots();
+}
+__device__ __forceinline__ long long part_row(const PagedAttnLaunch& a, const Item& it, int chunk, int kvh) {
+  return ((long long)part_slot(it, chunk) * a.hkv + (long long)kvh * it.slots()) * a.tile_rows;
+}
+// Prefix sums that go backwards can ask for more room than the batch's rows do; what has none is left out.
+__device__ __forceinline__ bool has_room(const PagedAttnLaunch& a, const Item& it) {
+  return it.n_chunks == 1 || part_slot(it, it.n_chunks - 1) + it.slots() <= a.max_slots;
+}
 
 // Where the keys and values of a sequence's KV head lie.
 template <bool PAGED>
@@ -151,7 +187,7 @@ __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item&
   for (int e = 0; e < CPL; ++e) o[e] *= inv;
   const float lse = m + logf(l);
   if (it.n_chunks > 1) {
-    const long long at = ((long long)part_of(it, it.chunk) * a.hkv + src.kvh) * a.tile_rows + row;
+    const long long at = part_row(a, it, it.chunk, src.kvh) + row;
     for (int e = 0; e < CPL; ++e) a.part_o[at * D + lane + 64 * e] = o[e];
     if (lane == 0) a.part_lse[at] = lse * kLog2e;
     return;
