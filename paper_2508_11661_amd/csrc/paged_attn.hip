@@ -22,9 +22,8 @@ template <int D, int NW>
 struct FewCfg {
   static constexpr int ROWB = D * 2, CPR = ROWB / 16, RPI = 1024 / ROWB;  // bytes and chunks per row, rows per request
   static constexpr int BK = 8192 / ROWB, NI = 8;                          // keys and requests of a tile
-  static constexpr int OROW = D * 4 + 16;                                 // bytes of an output row while the waves are joined
-  static constexpr int AREA = 32 * OROW > 16384 ? 32 * OROW : 16384;      // of a wave: K slot and V slot, then its output rows
-  static constexpr int STATS = NW * AREA, LDS_BYTES = STATS + NW * (32 * 8 + 4);
+  static constexpr int AREA = join_area(D) > 16384 ? join_area(D) : 16384;  // of a wave: K slot and V slot, then its output rows
+  static constexpr int LDS_BYTES = join_lds(NW, AREA);
   static __device__ __forceinline__ int kswz(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
   static __device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 };
@@ -211,80 +210,7 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
     }
   }
 
-  // join the waves: maxima and sums first, then the rows, each wave's scaled to the common maximum
-  float* s_m = reinterpret_cast<float*>(smem + C::STATS);
-  float* s_l = s_m + NW * 32;
-  int* s_bad = reinterpret_cast<int*>(s_l + NW * 32);
-  const bool bad = __any(most[0] >= 0x7F80 || most[1] >= 0x7F80);
-  const float l_row = sum_across_halves(l_run);
-  if (h == 0) {
-    s_m[wave * 32 + rw] = m_run;
-    s_l[wave * 32 + rw] = l_row;
-  }
-  if (lane == 0) s_bad[wave] = bad;
-  __syncthreads();
-  const int n_valid = min(32, n_rows - r0);
-  bool any_bad = false;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) any_bad |= s_bad[w] != 0;
-  if (any_bad) {
-    for (int row = wave; row < n_valid; row += NW) attend_row<true, D, PAGED>(a, it, src, r0 + row, begin, row);
-    return;
-  }
-  auto joined = [&](int row, float* m_out) {
-    float m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) m = fmaxf(m, s_m[w * 32 + row]);
-    const float m_use = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) l = fmaf(s_l[w * 32 + row], __builtin_amdgcn_exp2f(s_m[w * 32 + row] - m_use), l);
-    *m_out = m;
-    return l;
-  };
-  {
-    float m;
-    joined(rw, &m);
-    const float f = __builtin_amdgcn_exp2f(m_run - (m == -INFINITY ? 0.f : m));
-    char* mine = smem + wave * C::AREA + rw * C::OROW + h * 16;
-    if (rw < n_valid) {
-#pragma unroll
-      for (int dvb = 0; dvb < NV; ++dvb)
-#pragma unroll
-        for (int j4 = 0; j4 < 4; ++j4) {
-          f32x4 x;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = o[dvb][4 * j4 + e] * f;
-          *reinterpret_cast<f32x4*>(mine + (dvb * 32 + 8 * j4) * 4) = x;
-        }
-    }
-  }
-  __syncthreads();
-  constexpr int LPR = D / 4;
-  for (int row = threadIdx.x / LPR; row < n_valid; row += NW * 64 / LPR) {
-    const int c4 = threadIdx.x % LPR;
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(smem + w * C::AREA + row * C::OROW + c4 * 16);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] += y[e];
-    }
-    float m;
-    const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] *= inv;
-    const float lse2 = m + __log2f(l);
-    if (it.n_chunks > 1) {
-      const long long at = part_row(a, it, it.chunk, kvh) + row;
-      *reinterpret_cast<f32x4*>(a.part_o + at * D + c4 * 4) = x;
-      if (c4 == 0) a.part_lse[at] = lse2;
-    } else {
-      const int rr = r0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
-      const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
-      *reinterpret_cast<bf16x4*>(a.out.p + hd * a.out.hs + tok * a.out.rs + c4 * 8) = y;
-      if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = lse2 * kLn2;
-    }
-  }
+  join_waves<D, NW, true, PAGED, C::AREA>(a, it, src, o, m_run, l_run, __any(most[0] >= 0x7F80 || most[1] >= 0x7F80), begin);
 }
 
 template <int D, bool PAGED>
@@ -619,134 +545,7 @@ __global__ __launch_bounds__(512, 2) void k_attend_mixed(PagedAttnLaunch a) {
   else attend_few<D, PAGED, 8>(a, it, kvh);
 }
 
-// out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
-// four channels a lane).
-template <int D, bool BF16, bool WIDE>
-__global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
-  constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
-  const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
-  const int kvh = blockIdx.x % a.hkv;
-  int rows32 = 0;
-  const Item it = find_item<WIDE, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
-  if (it.s < 0 || !has_room(a, it)) return;
-  const int tile0 = it.tile * 32 * it.slots(), n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
-  for (int row = rows32 * 32 + uniform(blockIdx.y * 4 + (threadIdx.x >> 6)); row < n_rows; row += 4 * gridDim.y) {
-  const int rr = tile0 + row;
-  const int c4 = lane % LPR, cg = lane / LPR;
-  auto at = [&](int c) { return part_row(a, it, c, kvh) + row; };
-  float m = -INFINITY, den = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int c0 = 0; c0 < it.n_chunks; c0 += 64) {
-    const float l = c0 + lane < it.n_chunks ? a.part_lse[at(c0 + lane)] : -INFINITY;
-    float mx = l;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
-    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(m - m_use), wt = __builtin_amdgcn_exp2f(l - m_use);
-    float sum = wt;
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
-    den = fmaf(den, alpha, sum);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] *= alpha;
-    m = m_new;
-    const int n = min(64, it.n_chunks - c0);
-    constexpr int U = 4;  // requests ahead
-    for (int c = 0; c < n; c += U * CG) {
-      f32x4 x[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at(c0 + min(c + u * CG + cg, n - 1)) * D + c4 * 4);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int mine = c + u * CG + cg;
-        const float f = __shfl(wt, min(mine, 63));
-        if (mine < n) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, x[u][e], acc[e]);
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int w = LPR; w < 64; w *= 2)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], w);
-  if (cg > 0) continue;
-  const float inv = den == 0.f ? 0.f : 1.f / den;
-  const int tok = it.q.first + rr / group, hd = kvh * group + rr % group;
-  char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
-  if constexpr (BF16) {
-    const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
-    *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
-  } else {
-    *reinterpret_cast<f32x4*>(out + c4 * 16) = acc * inv;
-  }
-  if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
-  }
-}
-
-// ---------------------------------------------------------------------------------------------- float32, and the host side
-template <bool BF16>
-__device__ __forceinline__ float element(const char* row, int c) {
-  if constexpr (BF16) return (float)reinterpret_cast<const __bf16*>(row)[c];
-  else return reinterpret_cast<const float*>(row)[c];
-}
-
-template <bool BF16, int D, bool PAGED>
-__global__ __launch_bounds__(256) void k_paged_attn(PagedAttnLaunch a) {
-  constexpr int CPL = D / 64;
-  const int lane = threadIdx.x & 63;
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), head = blockIdx.y;
-  if (row >= a.b.n_rows) return;
-  const int s = seq_of_row(a.b, row, lane);
-  if (s >= a.b.n_seq) return;
-  const SeqSpan q = seq_span(a.b, s);
-  const int t = row - q.first;
-  if (t < 0 || t >= q.n) return;
-  const int n_keys = q.len - q.n + t + 1, kvh = head / (a.hq / a.hkv);
-  auto at = [&](const RowsArg& r, int key) {
-    if constexpr (PAGED) {
-      const int page = min(max(a.b.table[(long long)s * a.b.max_pages + (key >> a.b.page_log2)], 0), a.b.n_pages - 1);
-      return r.p + ((long long)page * a.hkv + kvh) * r.hs + (key & ((1 << a.b.page_log2) - 1)) * r.rs;
-    } else {
-      return r.p + kvh * r.hs + (q.first + key) * r.rs;
-    }
-  };
-  const char* qr = a.q.p + head * a.q.hs + row * a.q.rs;
-  float m = -INFINITY, l = 0.f, o[CPL] = {};
-  for (int k0 = 0; k0 < n_keys; k0 += 64) {
-    float x = -INFINITY;
-    if (k0 + lane < n_keys) {
-      const char* kr = at(a.k, k0 + lane);
-      float dot = 0.f;
-      for (int c = 0; c < D; ++c) dot = fmaf(element<BF16>(qr, c), element<BF16>(kr, c), dot);
-      x = dot * a.scale;
-    }
-    float mx = x;
-    for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
-    const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-    const float p = expf(x - m_use), alpha = expf(m - m_use);
-    float sum = p;
-    for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
-    l = l * alpha + sum;
-    m = m_new;
-    for (int e = 0; e < CPL; ++e) o[e] *= alpha;
-    for (int j = 0; j < min(64, n_keys - k0); ++j) {
-      const float w = __shfl(p, j);
-      const char* vr = at(a.v, k0 + j);
-      for (int e = 0; e < CPL; ++e) o[e] = fmaf(w, element<BF16>(vr, lane + 64 * e), o[e]);
-    }
-  }
-  char* out = a.out.p + head * a.out.hs + row * a.out.rs;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int e = 0; e < CPL; ++e) {
-    if constexpr (BF16) reinterpret_cast<__bf16*>(out)[lane + 64 * e] = (__bf16)(o[e] * inv);
-    else reinterpret_cast<float*>(out)[lane + 64 * e] = o[e] * inv;
-  }
-  if (a.lse != nullptr && lane == 0) a.lse[(long long)head * a.b.n_rows + row] = m + logf(l);
-}
-
+// ---------------------------------------------------------------------------------------------- launches
 template <int D>
 constexpr int mixed_lds() {
   return WideCfg<D>::LDS_BYTES > FewCfg<D, 8>::LDS_BYTES ? WideCfg<D>::LDS_BYTES : FewCfg<D, 8>::LDS_BYTES;
@@ -759,18 +558,7 @@ hipError_t run_bf16(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_
   else hipLaunchKernelGGL((k_attend_few<D, PAGED>), grid, dim3(256), (FewCfg<D, 4>::LDS_BYTES), s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.joins) return e;
-  const dim3 join((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.wide ? 1 : (p.tile_rows + 3) / 4));
-  if (p.wide) hipLaunchKernelGGL((k_join_chunks<D, true, true>), join, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_join_chunks<D, true, false>), join, dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
-template <int D>
-hipError_t run_f32(const PagedAttnLaunch& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.b.n_rows + 3) / 4), (unsigned)a.hq);
-  if (a.paged) hipLaunchKernelGGL((k_paged_attn<false, D, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_paged_attn<false, D, false>), grid, dim3(256), 0, s, a);
-  return hipGetLastError();
+  return launch_join<D, true>(a, p, s);
 }
 
 template <int D, bool PAGED>
@@ -791,7 +579,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   p.target = p.wide ? 256 : 512;  // as many workgroups as are resident at once
   p.min_chunk = 256;
   // Prompts that fill the chip many times over are not cut: the join would be one more launch.
-  p.joins = dtype == SAMKV_BF16 && max_len > p.min_chunk && (paged || rows / kWideRows * hkv < 4 * p.target);
+  p.joins = max_len > p.min_chunk && (paged || rows / kWideRows * hkv < 4 * p.target);
   // Items: the tiles of 32 rows that there can be, or of 256 and those of sequences with few rows, and the chunks that find_item
   // cuts (a chunk holds at least 1 / target of the cost of all heads, and a tile's cost is at least half of its keys').
   const long long few_most = p.wide ? kFewRows : most, per = p.wide ? kWideRows / 32 : 1, shares = (p.target + hkv - 1) / hkv;
@@ -807,17 +595,18 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
 }
 
 hipError_t paged_attn_raise_limits() {
-  const hipError_t all[] = {raise_limit<128, true>(), raise_limit<128, false>(), raise_limit<64, true>(), raise_limit<64, false>()};
+  const hipError_t all[] = {raise_limit<128, true>(), raise_limit<128, false>(), raise_limit<64, true>(), raise_limit<64, false>(),
+                            paged_attn_f32_raise_limits()};
   for (hipError_t e : all)
     if (e != hipSuccess) return e;
   return hipSuccess;
 }
 
 hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s) {
-  if (a.dtype != SAMKV_BF16) return a.d == 128 ? run_f32<128>(a, s) : run_f32<64>(a, s);
   const hipError_t e = attn_prepare_device();
   if (e != hipSuccess) return e;
   const PagedAttnPlan p = paged_attn_plan(a.dtype, a.d, a.hq, a.hkv, a.b.n_seq, a.b.n_rows, a.b.max_new, a.b.max_len, a.paged != 0);
+  if (a.dtype != SAMKV_BF16) return launch_paged_attn_f32(a, p, s);
   if (a.paged) return a.d == 128 ? run_bf16<128, true>(a, p, s) : run_bf16<64, true>(a, p, s);
   return a.d == 128 ? run_bf16<128, false>(a, p, s) : run_bf16<64, false>(a, p, s);
 }

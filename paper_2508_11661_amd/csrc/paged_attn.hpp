@@ -200,4 +200,177 @@ __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item&
   if (a.lse != nullptr && lane == 0) a.lse[(long long)head * a.b.n_rows + tok] = lse;
 }
 
+// Joins the partial results of NW waves over one tile of 32 rows and writes them (as the item's, or as a part of them): maxima
+// and sums first, then the rows, each wave's scaled to the common maximum, through LDS.  `bad`: the wave has met an infinity or a
+// NaN among its values.
+constexpr int join_area(int d) { return 32 * (d * 4 + 16); }  // LDS bytes of a wave's rows (pad: 16 rows hit 64 distinct banks)
+constexpr int join_lds(int nw, int area) { return nw * area + nw * (32 * 8 + 4); }
+template <int D, int NW, bool BF16, bool PAGED, int AREA>
+__device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item& it, const KvSource<PAGED>& src, f32x16 (&o)[D / 32],
+                                           float m_run, float l_run, bool bad, int begin) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  constexpr int NV = D / 32, OROW = D * 4 + 16;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), rw = lane & 31, h = lane >> 5;
+  const int group = a.hq / a.hkv, kvh = src.kvh, n_rows = it.q.n * group, r0 = it.tile * 32;
+  float* s_m = reinterpret_cast<float*>(smem + NW * AREA);
+  float* s_l = s_m + NW * 32;
+  int* s_bad = reinterpret_cast<int*>(s_l + NW * 32);
+  const float l_row = sum_across_halves(l_run);
+  if (h == 0) {
+    s_m[wave * 32 + rw] = m_run;
+    s_l[wave * 32 + rw] = l_row;
+  }
+  if (lane == 0) s_bad[wave] = bad;
+  __syncthreads();
+  const int n_valid = min(32, n_rows - r0);
+  bool any_bad = false;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) any_bad |= s_bad[w] != 0;
+  if (any_bad) {
+    for (int row = wave; row < n_valid; row += NW) attend_row<BF16, D, PAGED>(a, it, src, r0 + row, begin, row);
+    return;
+  }
+  auto joined = [&](int row, float* m_out) {
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, s_m[w * 32 + row]);
+    const float m_use = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l = fmaf(s_l[w * 32 + row], __builtin_amdgcn_exp2f(s_m[w * 32 + row] - m_use), l);
+    *m_out = m;
+    return l;
+  };
+  {
+    float m;
+    joined(rw, &m);
+    const float f = __builtin_amdgcn_exp2f(m_run - (m == -INFINITY ? 0.f : m));
+    char* mine = smem + wave * AREA + rw * OROW + h * 16;
+    if (rw < n_valid) {
+#pragma unroll
+      for (int dvb = 0; dvb < NV; ++dvb)
+#pragma unroll
+        for (int j4 = 0; j4 < 4; ++j4) {
+          f32x4 x;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = o[dvb][4 * j4 + e] * f;
+          *reinterpret_cast<f32x4*>(mine + (dvb * 32 + 8 * j4) * 4) = x;
+        }
+    }
+  }
+  __syncthreads();
+  constexpr int LPR = D / 4;
+  for (int row = threadIdx.x / LPR; row < n_valid; row += NW * 64 / LPR) {
+    const int c4 = threadIdx.x % LPR;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(smem + w * AREA + row * OROW + c4 * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] += y[e];
+    }
+    float m;
+    const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] *= inv;
+    const float lse2 = m + __log2f(l);
+    if (it.n_chunks > 1) {
+      const long long at = part_row(a, it, it.chunk, kvh) + row;
+      *reinterpret_cast<f32x4*>(a.part_o + at * D + c4 * 4) = x;
+      if (c4 == 0) a.part_lse[at] = lse2;
+    } else {
+      const int rr = r0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+      char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
+      if constexpr (BF16) {
+        const bf16x4 y = {(__bf16)x[0], (__bf16)x[1], (__bf16)x[2], (__bf16)x[3]};
+        *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
+      } else {
+        *reinterpret_cast<f32x4*>(out + c4 * 16) = x;
+      }
+      if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = lse2 * kLn2;
+    }
+  }
+}
+
+// out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
+// four channels a lane).
+template <int D, bool BF16, bool WIDE>
+__global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
+  constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
+  const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
+  const int kvh = blockIdx.x % a.hkv;
+  int rows32 = 0;
+  const Item it = find_item<WIDE, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
+  if (it.s < 0 || !has_room(a, it)) return;
+  const int tile0 = it.tile * 32 * it.slots(), n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
+  for (int row = rows32 * 32 + uniform(blockIdx.y * 4 + (threadIdx.x >> 6)); row < n_rows; row += 4 * gridDim.y) {
+    const int rr = tile0 + row;
+    const int c4 = lane % LPR, cg = lane / LPR;
+    auto at = [&](int c) { return part_row(a, it, c, kvh) + row; };
+    float m = -INFINITY, den = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int c0 = 0; c0 < it.n_chunks; c0 += 64) {
+      const float l = c0 + lane < it.n_chunks ? a.part_lse[at(c0 + lane)] : -INFINITY;
+      float mx = l;
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
+      const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = __builtin_amdgcn_exp2f(m - m_use), wt = __builtin_amdgcn_exp2f(l - m_use);
+      float sum = wt;
+#pragma unroll
+      for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
+      den = fmaf(den, alpha, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+      m = m_new;
+      const int n = min(64, it.n_chunks - c0);
+      constexpr int U = 4;  // requests ahead
+      for (int c = 0; c < n; c += U * CG) {
+        f32x4 x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at(c0 + min(c + u * CG + cg, n - 1)) * D + c4 * 4);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int mine = c + u * CG + cg;
+          const float f = __shfl(wt, min(mine, 63));
+          if (mine < n) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, x[u][e], acc[e]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int w = LPR; w < 64; w *= 2)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], w);
+    if (cg > 0) continue;
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    const int tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+    char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
+    if constexpr (BF16) {
+      const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+      *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
+    } else {
+      f32x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = acc[e] * inv;
+      *reinterpret_cast<f32x4*>(out + c4 * 16) = y;
+    }
+    if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
+  }
+}
+
+template <int D, bool BF16>
+hipError_t launch_join(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
+  // a tile that is cut has two slots at least
+  const dim3 grid((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.wide ? 1 : (p.tile_rows + 3) / 4));
+  if (p.wide) hipLaunchKernelGGL((k_join_chunks<D, BF16, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_join_chunks<D, BF16, false>), grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_attn_f32(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s);
+hipError_t paged_attn_f32_raise_limits();
+
 }  // namespace samkv
