@@ -28,6 +28,11 @@ struct FewCfg {
   static __device__ __forceinline__ int vswz(int row) { return D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1); }
 };
 
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* lds_at(uint32_t at) {
+  return (__attribute__((address_space(3))) T*)(size_t)at;
+}
+
 // Lane L of a wave-wide request lands at lds + 16 L.
 __device__ __forceinline__ void request(const char* base, uint32_t off, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "memory", "m0");
@@ -273,7 +278,11 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
   const KvSource<PAGED> src{a, it.s, kvh, it.q.first, it.q.len - 1};
   const uint32_t smem_at = (uint32_t)(size_t)(const __attribute__((address_space(3))) char*)smem;
   const uint32_t wave_rows = uniform(smem_at + NI * wave * 1024);
-  const int key0 = begin + 8 * wave;
+  const int lrow = lane / CPR, key0 = begin + 8 * wave;
+  uint32_t k_chunk[NI], v_chunk;  // the swizzle of V is that of a request's first row in all of them
+#pragma unroll
+  for (int i = 0; i < NI; ++i) k_chunk[i] = (uint32_t)((lane % CPR) ^ F::kswz(8 * wave + i * C::RPI + lrow)) * 16;
+  v_chunk = (uint32_t)((lane % CPR) ^ F::vswz(lrow)) * 16;
   int pages = 0;
   auto look_up = [&](int j) {
     if constexpr (PAGED) {
@@ -283,44 +292,38 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
   };
   auto page_of = [&](int j) { return PAGED ? __builtin_amdgcn_readlane(pages, j & 63) : 0; };
   auto request_rows = [&](const RowsArg& rows, bool is_v, int j, int page, uint32_t slot) {
-    const int key = key0 + j * BK;
-    const char* base = rows.p + src.at(rows, min(key, src.last), page);
-    const int lim = max(src.last - key, 0);
-    int l = lane;
-    asm volatile("" : "+v"(l));  // offsets are made here, not kept in registers
-    const int lrow = l / CPR, pos = l % CPR;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int row = i * C::RPI + lrow;
-      const uint32_t chunk = (uint32_t)(pos ^ (is_v ? F::vswz(row) : F::kswz(8 * wave + row))) * 16;
-      request(base, (uint32_t)min(row, lim) * (uint32_t)rows.rs + chunk, wave_rows + slot + i * 1024);
+      const int key = key0 + j * BK + i * C::RPI, lim = max(src.last - key, 0);
+      request(rows.p + src.at(rows, min(key, src.last), page),
+              (uint32_t)min(lrow, lim) * ((uint32_t)rows.rs & 0xFFFFFFu) + (is_v ? v_chunk : k_chunk[i]), wave_rows + slot + i * 1024);
     }
   };
-  auto k_off = [&](int j) { return (uint32_t)((j % 3) * TILE); };
-  auto v_off = [&](int j) { return (uint32_t)((3 + j % 3) * TILE); };
-  auto request_k = [&](int j, int page) { request_rows(a.k, false, j, page, k_off(j)); };
-  auto request_v = [&](int j, int page) { request_rows(a.v, true, j, page, v_off(j)); };
+  // Requests never depend on whether there is a tile to request: past the last one it is requested again, into a slot that
+  // nobody reads any more, and every step has the same number on their way.
+  auto request_k = [&](int j, int page, uint32_t slot) { request_rows(a.k, false, min(j, n_tiles - 1), page, slot); };
+  auto request_v = [&](int j, int page, uint32_t slot) { request_rows(a.v, true, min(j, n_tiles - 1), page, 3 * TILE + slot); };
 
-  // ---- fragments: LDS addresses of the first one in slot 0; the others differ in bits that an exclusive or turns (slots are
-  // multiples of 1 KB).  Made where they are used: kept, they would cost registers that the two sets of scores need.
-  const uint32_t k_at = (uint32_t)(rw * ROWB + ((h ^ F::kswz(rw)) * 16));
+  // ---- fragments: LDS addresses of the first one in slot 0; the others differ in bits that an exclusive or turns (slots, and the
+  // ring, start at multiples of 1 KB).  Made where they are used: kept, they would cost registers that the two sets of scores need.
+  const uint32_t k_at = smem_at + (uint32_t)(rw * ROWB + ((h ^ F::kswz(rw)) * 16));
   uint32_t v_at;
   {
     const int i16 = lane & 15, q2 = (lane >> 4) & 1, vrow = 4 * h + (i16 >> 2);
-    v_at = (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ F::vswz(vrow)) * 16) + 8 * (i16 & 1));
+    v_at = smem_at + 3 * TILE + (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ F::vswz(vrow)) * 16) + 8 * (i16 & 1));
   }
   auto kfrags = [&](uint32_t slot, int kb, bf16x8 (&ak)[ND]) {
     uint32_t at = k_at + slot;
     asm volatile("" : "+v"(at));
 #pragma unroll
-    for (int dc = 0; dc < ND; ++dc) ak[dc] = *reinterpret_cast<const bf16x8*>(smem + (at ^ (dc << 5)) + kb * 32 * ROWB);
+    for (int dc = 0; dc < ND; ++dc) ak[dc] = *lds_at<bf16x8>((at ^ (dc << 5)) + kb * 32 * ROWB);
   };
   auto vfrags = [&](uint32_t at, int g, Frag (&av)[NV]) {
 #pragma unroll
     for (int dvb = 0; dvb < NV; ++dvb) {
-      const char* vp = smem + (at ^ (dvb << 6)) + g * 16 * ROWB;
-      av[dvb].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp));
-      av[dvb].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vp + 8 * ROWB));
+      const uint32_t vp = (at ^ (dvb << 6)) + g * 16 * ROWB;
+      av[dvb].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp));
+      av[dvb].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp + 8 * ROWB));
     }
   };
 
@@ -414,84 +417,139 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
 
   if (n_tiles > 0) {
     look_up(0);
-    int page_v = 0, page_k = page_of(0);
-    request_k(0, page_k);
-    request_v(0, page_k);
-    if (n_tiles > 1) {
-      page_k = page_of(1);
-      request_k(1, page_k);
-      request_v(1, page_k);
-    }
-    if (n_tiles > 2) {
-      page_k = page_of(2);
-      request_k(2, page_k);
-    }
-    // K(0) for the first scores
-    if (n_tiles > 2) wait_loads<4 * NI>();
-    else if (n_tiles > 1) wait_loads<3 * NI>();
-    else wait_loads<NI>();
+    int page_k = page_of(0), page_v;
+    request_k(0, page_k, 0);
+    request_v(0, page_k, 0);
+    page_k = page_of(min(1, n_tiles - 1));
+    request_k(1, page_k, TILE);
+    request_v(1, page_k, TILE);
+    page_k = page_of(min(2, n_tiles - 1));
+    request_k(2, page_k, 2 * TILE);
+    wait_loads<4 * NI>();  // K(0) for the first scores
     __builtin_amdgcn_s_barrier();
     f32x16 sA[2], sB[2];
     scores(0, sA);
     // V(0) and K(1) for step 0; K(0) has been read by every wave before step 0 requests its slot's next tile
-    if (n_tiles > 2) wait_loads<2 * NI>();
-    else if (n_tiles > 1) wait_loads<NI>();
-    else wait_loads<0>();
+    wait_loads<2 * NI>();
     wait_lds();
     __builtin_amdgcn_s_barrier();
 
-    // Every wave walks all tiles: it requests its rows and meets the barriers, whatever it computes.
-    auto ahead = [&](int tile) {
+    // Every wave walks all tiles: it requests its rows and meets the barriers, whatever it computes.  Step t requests K(t + 3)
+    // into the slot of K(t), which step t - 1 has read, and V(t + 2) into that of V(t - 1).
+    int tile = 0;
+    uint32_t s0 = 0, s1 = TILE, s2 = 2 * TILE;  // slots of tiles t, t + 1, t + 2
+    auto ahead_k = [&]() {
       page_v = page_k;
-      if (tile + 3 < n_tiles) {
-        if (PAGED && ((tile + 3) & 63) == 0) look_up(tile + 3);
-        page_k = page_of(tile + 3);
-        request_k(tile + 3, page_k);
-      }
-      if (tile + 2 < n_tiles) request_v(tile + 2, page_v);
+      if (PAGED && ((tile + 3) & 63) == 0 && tile + 3 < n_tiles) look_up(tile + 3);
+      page_k = page_of(min(tile + 3, n_tiles - 1));
+      request_k(tile + 3, page_k, s0);
     };
-    auto done = [&](int tile) {  // the next step's tiles were requested one step ago: all but this step's requests have to land
-      if (tile + 3 < n_tiles) wait_loads<2 * NI>();
-      else if (tile + 2 < n_tiles) wait_loads<NI>();
-      else wait_loads<0>();
+    auto ahead_v = [&]() { request_v(tile + 2, page_v, s2); };
+    auto done = [&]() {  // the next step's tiles were requested one step ago: all but this step's requests have to land
+      wait_loads<2 * NI>();
       wait_lds();
       __builtin_amdgcn_s_barrier();
+      const uint32_t s = s0;
+      s0 = s1;
+      s1 = s2;
+      s2 = s;
+      ++tile;
     };
-    // unmasked tiles, two at a time: S(tile) is in sc, S(tile + 1) goes to sn
-    auto step = [&](int tile, f32x16 (&sc)[2], f32x16 (&sn)[2]) {
-      ahead(tile);
-      const uint32_t k_next = k_off(tile + 1);
-      bf16x8 ak0[ND], ak1[ND];
-      kfrags(k_next, 0, ak0);
-      lift(row_max(sc));
-      kfrags(k_next, 1, ak1);
+    // Unmasked tiles, two at a time: S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The
+    // order of the instructions is fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier):
+    // a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
+    // use, and the maximum of the new scores under the last products.
+    float mx = 0.f;
+    auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+      constexpr int NS = 2 * ND, NP = 4 * NV;  // products of S and of O
+      uint32_t ks = k_at + s1, vs = v_at + s0;
+      asm volatile("" : "+v"(ks), "+v"(vs));
+      bf16x8 ak[ND], bp[4];
+      Frag va[2 * NV];
+      float psum = 0.f;
+      auto k_read = [&](int i) {
+        ak[i % ND] = *lds_at<bf16x8>((ks ^ ((i % ND) << 5)) + (i / ND) * 32 * ROWB);
+      };
+      auto v_read = [&](int j) {
+        const uint32_t vp = (vs ^ ((j % NV) << 6)) + (j / NV) * 16 * ROWB;
+        va[j % (2 * NV)].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp));
+        va[j % (2 * NV)].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp + 8 * ROWB));
+      };
 #pragma unroll
-      for (int j = 0; j < 16; ++j) { sn[0][j] = 0.f; sn[1][j] = 0.f; }
+      for (int i = 0; i < ND; ++i) k_read(i);
+      lift(mx);
+      const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
+      auto pair = [&](int k) {  // weights 2 k and 2 k + 1 of the lane
+        const int g = k / 4, e = 2 * (k % 4);
+        const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e], c2, -m_use));
+        const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e + 1], c2, -m_use));
+        bp[g][e] = (__bf16)p0;
+        bp[g][e + 1] = (__bf16)p1;
+        psum += p0 + p1;
+        asm volatile("" : : "v"(psum));  // here, not where the sum is used
+      };
 #pragma unroll
-      for (int dc = 0; dc < ND; ++dc) sn[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak0[dc], bq[dc], sn[0], 0, 0, 0);
+      for (int k = 0; k < 4; ++k) pair(k);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int dc = 0; dc < ND; ++dc) sn[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak1[dc], bq[dc], sn[1], 0, 0, 0);
-      weights_pv(sc, v_off(tile), false);
-      done(tile);
+      for (int i = 0; i < NS; ++i) {
+        if (i % ND == 0) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) sn[i / ND][j] = 0.f;
+        }
+        sn[i / ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[i % ND], bq[i % ND], sn[i / ND], 0, 0, 0);
+        if (i < ND) k_read(i + ND);
+        else if (i - ND < 2 * NV) v_read(i - ND);
+        if ((i + 1) * 8 / NS > i * 8 / NS) pair(4 + i * 8 / NS);
+        if (i == NS / 4) ahead_k();
+        if (i == NS / 2) ahead_v();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        o[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j % (2 * NV)].b, bp[j / NV], o[j % NV], 0, 0, 0);
+        if (j + 2 * NV < NP) v_read(j + 2 * NV);
+        constexpr int EARLY = NP / 4, PER = 4 / EARLY > 0 ? 4 / EARLY : 1, MAXES = (32 / (NP - EARLY) + 2) / 2 * 2;  // pairs: one instruction takes two
+        if (j < EARLY) {
+#pragma unroll
+          for (int k = 0; k < PER; ++k) pair(12 + j * PER + k);
+        } else {
+#pragma unroll
+          for (int k = 0; k < MAXES; ++k) {
+            const int v = (j - EARLY) * MAXES + k;
+            if (v < 32) top = fmaxf(top, sn[v / 16][v % 16]);
+          }
+          asm volatile("" : : "v"(top));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l_run += psum;
+      mx = max_across_halves(top) * c2;
+      done();
     };
-    int tile = 0;
-    for (; tile + 1 < n_full; tile += 2) {
-      step(tile, sA, sB);
-      step(tile + 1, sB, sA);
+    if (n_full > 1) mx = row_max(sA);
+    while (tile + 1 < n_full) {
+      step(sA, sB);
+      step(sB, sA);
     }
     // the masked ones behind them, and an odd unmasked one
-    for (; tile < n_any; ++tile) {
-      ahead(tile);
+    while (tile < n_any) {
+      ahead_k();
+      ahead_v();
       mask(tile, sA);
       lift(row_max(sA));
-      weights_pv(sA, v_off(tile), true);
-      if (tile + 1 < n_any) scores(k_off(tile + 1), sA);
-      done(tile);
+      weights_pv(sA, s0, true);
+      if (tile + 1 < n_any) scores(s1, sA);
+      done();
     }
-    for (; tile < n_tiles; ++tile) {
-      ahead(tile);
-      done(tile);
+    while (tile < n_tiles) {
+      ahead_k();
+      ahead_v();
+      done();
     }
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();  // the ring is free for the output rows once nobody's requests are on their way
   }
 
   if (!has_rows) return;
@@ -522,7 +580,7 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       *reinterpret_cast<bf16x4*>(turn + rw * RS + (dvb * 32 + 8 * j4 + 4 * h) * 2) = y;
     }
   const int r_end = min(r0 + rw_end, n_rows - 1);
-  const int head = kvh * group + r_end % group, tok = it.q.first + r_end / group, lrow = lane / CPR, pos = lane % CPR;
+  const int head = kvh * group + r_end % group, tok = it.q.first + r_end / group, pos = lane % CPR;
   const long long to = head * a.out.hs + tok * a.out.rs;
   __builtin_amdgcn_wave_barrier();
 #pragma unroll

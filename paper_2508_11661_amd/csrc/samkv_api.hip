@@ -1061,7 +1061,7 @@ int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_row
   if ((rc = check_rows(k, n_kv_heads, n_tok, head_dim, dtype, false, &a.k)) != SAMKV_OK) return rc;
   if ((rc = check_rows(v, n_kv_heads, n_tok, head_dim, dtype, false, &a.v)) != SAMKV_OK) return rc;
   if ((rc = check_rows(out, n_q_heads, n_tok, head_dim, dtype, true, &a.out)) != SAMKV_OK) return rc;
-  if (a.k.rs > (1 << 27) || a.v.rs > (1 << 27)) return SAMKV_EUNSUPPORTED;  // rows of a tile are told apart by 32-bit offsets
+  if (a.k.rs >= (1 << 24) || a.v.rs >= (1 << 24)) return SAMKV_EUNSUPPORTED;  // rows of a tile are told apart by 24-bit products
   a.dtype = dtype; a.d = head_dim; a.hq = n_q_heads; a.hkv = n_kv_heads; a.paged = 0;
   a.b.n_seq = n_seq; a.b.n_rows = n_tok; a.b.max_new = a.b.max_len = max_len < n_tok ? max_len : n_tok;
   a.b.cu = cu;
