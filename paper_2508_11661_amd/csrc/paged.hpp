@@ -83,7 +83,7 @@ hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
 
 // Sizes of a launch that follow from the bounds alone.
 struct PagedAttnPlan {
-  bool wide;   // whether any sequence can have more than kFewRows rows per KV head and a kernel for them
+  int kg;  // which wide tiles there are: see paged_attn.hpp
   int target, min_chunk, max_items, max_slots, tile_rows;
   bool joins;  // whether any sequence can have more than one chunk
   size_t part_lse, bytes;  // workspace: part_o, then part_lse

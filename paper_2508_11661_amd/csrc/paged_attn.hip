@@ -48,12 +48,6 @@ union Frag {
   bf16x8 b;
   u32x4 u;
 };
-// The larger magnitudes, half by half, as bit patterns: 0x7F80 and above are infinities and NaN.
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ u16x2 larger_magnitude(u16x2 m, uint32_t x) {
-  return __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, x & 0x7FFF7FFFu));
-}
-
 template <int D, bool PAGED, int NW>
 __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item& it, int kvh) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -116,7 +110,6 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m_run = -INFINITY, l_run = 0.f;
-  u16x2 most = {0, 0};  // magnitude of V
   const float c2 = a.scale * kLog2e;
 
   int k0 = begin + wave * C::BK;
@@ -204,10 +197,6 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
         if (more) request_tile(k1, pg, a.v, true, v_lds);
       }
 #pragma unroll
-      for (int dvb = 0; dvb < NV; ++dvb)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) most = larger_magnitude(most, av[dvb].u[e]);
-#pragma unroll
       for (int dvb = 0; dvb < NV; ++dvb) {
         o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[dvb].b, bhi[g], o[dvb], 0, 0, 0);
         o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(av[dvb].b, blo[g], o[dvb], 0, 0, 0);
@@ -215,78 +204,80 @@ __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item&
     }
   }
 
-  join_waves<D, NW, true, PAGED, C::AREA>(a, it, src, o, m_run, l_run, __any(most[0] >= 0x7F80 || most[1] >= 0x7F80), begin);
+  join_waves<D, NW, true, PAGED, C::AREA>(a, it, src, o, m_run, l_run, begin);
 }
 
 template <int D, bool PAGED>
 __global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
   const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<false, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  const Item it = find_item<0, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
   if (it.s < 0 || !has_room(a, it)) return;
   attend_few<D, PAGED, 4>(a, it, kvh);
 }
 
 // ---------------------------------------------------------------------------------------------- many rows
-// Eight waves of 32 rows each, one workgroup per compute unit; tiles of 64 keys that all waves read.  K and V tiles travel
-// straight into a ring of three LDS slots each, requested two steps ahead of their use.  Inside a wave the products of the next
-// tile's scores are issued in one block with the weights of the current one, so that the matrix unit and the vector unit work at
-// the same time:
+// Eight waves of 32 rows each, one workgroup per compute unit; tiles of keys that the waves share.  K and V tiles travel straight
+// into a ring of LDS slots.  Inside a wave the products of the next tile's scores are issued among the weights of the current one,
+// so that the matrix unit and the vector unit work at the same time:
 //     step t:  S(t+1) = K(t+1) Q^T (matrix)  |  P(t) = 2^(S(t) c - m) (vector);  O^T += V(t)^T P(t)^T (matrix)
 // The running maximum is raised only when a row outgrows it by 2^8, which keeps the rescaling of O off the common path: weights
 // stay below 256.  They are rounded to bf16 (half a step, 2^-8 relative, as the output is in the end); their sum is that of the
 // unrounded weights, in float32.
-template <int D>
+// KG = 1: 256 rows and 64 keys a step, tiles requested two steps ahead.  KG = 2, where 256 rows at a time would leave compute
+// units idle or the longest tile's chain of steps would last: 128 rows, and 128 keys a step of which either half of the waves
+// takes 64; the halves meet through LDS at the end.
+template <int D, int KG>
 struct WideCfg {
-  static constexpr int NW = 8, BK = 64, NSLOT = 3;
+  static constexpr int NW = 8, RG = NW / KG, BK = 64, BKT = BK * KG;    // waves, row groups, keys per wave and per step
+  static constexpr int NSLOT = KG == 2 && D == 128 ? 2 : 3;             // K is requested NSLOT tiles ahead, V one less
   static constexpr int ROWB = D * 2, CPR = ROWB / 16, RPI = 1024 / ROWB;
-  static constexpr int TILE = BK * ROWB, NI = TILE / 1024 / NW;  // a wave requests 8 rows of a tile, which lie in one page
+  static constexpr int TILE = BKT * ROWB, NI = TILE / 1024 / NW;        // a wave requests 8 KG rows of a tile, which lie in one page
+  static constexpr int MERGE = 64 * (D / 2 + 2) * 4;                    // one wave's outputs, maxima and sums
   static constexpr int LDS_BYTES = 2 * NSLOT * TILE;
-  static_assert(NI * RPI == 8, "rows of a wave");
+  static constexpr int AHEAD = NSLOT == 3 ? 2 * NI : 0;                 // requests that may be on their way at a step's end
+  static_assert(NI * RPI == 8 * KG, "rows of a wave");
 };
 
-template <int D, bool PAGED>
+template <int D, bool PAGED, int KG>
 __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item& it, int kvh) {
-  using C = WideCfg<D>;
+  using C = WideCfg<D, KG>;
   using F = FewCfg<D, 8>;  // the swizzles
-  constexpr int ND = D / 16, NV = D / 32, ROWB = C::ROWB, CPR = C::CPR, NI = C::NI, TILE = C::TILE, BK = C::BK;
+  constexpr int ND = D / 16, NV = D / 32, ROWB = C::ROWB, CPR = C::CPR, NI = C::NI, TILE = C::TILE, NSLOT = C::NSLOT;
+  constexpr int BK = C::BK, BKT = C::BKT, ROWS = wide_rows<KG>();
   constexpr float TAU = 8.f;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  // K(j) in slot j % 3 at smem + slot * TILE, V(j) at smem + (3 + slot) * TILE
+  // K(j) in slot j % NSLOT at smem + slot * TILE, V(j) at smem + (NSLOT + slot) * TILE
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int rw = lane & 31, h = lane >> 5;
-  const int group = a.hq / a.hkv, n_rows = it.q.n * group, r0 = it.tile * kWideRows + wave * 32;
+  const int rw = lane & 31, h = lane >> 5, rg = wave % C::RG, key_g = wave / C::RG * BK;
+  const int group = a.hq / a.hkv, n_rows = it.q.n * group, r0 = it.tile * ROWS + rg * 32;
   const int pos0 = it.q.len - it.q.n;
   auto slots_seen = [&](int r) { return min(pos0 + min(r, n_rows - 1) / group + 1, it.q.len); };  // keys that row r sees
 
   const int begin = it.chunk * it.c;
-  const int end = min(slots_seen(it.tile * kWideRows + kWideRows - 1), begin + it.c);
-  const int n_tiles = max((end - begin + BK - 1) / BK, 0);
+  const int end = min(slots_seen(it.tile * ROWS + ROWS - 1), begin + it.c);
+  const int n_tiles = max((end - begin + BKT - 1) / BKT, 0);
   const bool has_rows = r0 < n_rows;
-  const int seen_first = has_rows ? min(slots_seen(r0), end) : begin, seen_last = has_rows ? min(slots_seen(r0 + 31), end) : begin;
-  const int n_full = max(seen_first - begin, 0) / BK, n_any = max(seen_last - begin + BK - 1, 0) / BK;  // unmasked tiles; tiles
+  // tiles whose keys of this wave the first row sees all, and tiles of which the last row sees any
+  const int seen_first = has_rows ? min(slots_seen(r0), end) - begin - key_g : 0;
+  const int seen_last = has_rows ? min(slots_seen(r0 + 31), end) - begin - key_g : 0;
+  const int n_full = max(seen_first + BKT - BK, 0) / BKT, n_any = max(seen_last + BKT - 1, 0) / BKT;
 
-  const int r = min(r0 + rw, n_rows - 1);
-  const int key_end = min(slots_seen(r), end);
   bf16x8 bq[ND];
-  {
-    const char* qp = a.q.p + (kvh * group + r % group) * a.q.hs + (long long)(it.q.first + r / group) * a.q.rs + h * 16;
-#pragma unroll
-    for (int dc = 0; dc < ND; ++dc) bq[dc] = *reinterpret_cast<const bf16x8*>(qp + dc * 32);
-  }
+  int key_end;  // one past the last key that counts for this lane's row, in the wave's keys
 
-  // ---- requests: rows 8 wave .. 8 wave + 7 of every tile.  The pages of 64 tiles are looked up at once, one per lane.
+  // ---- requests: rows 8 KG wave .. 8 KG wave + 8 KG - 1 of every tile.  The pages of 64 tiles are looked up at once, one per
+  // lane.
   const KvSource<PAGED> src{a, it.s, kvh, it.q.first, it.q.len - 1};
   const uint32_t smem_at = (uint32_t)(size_t)(const __attribute__((address_space(3))) char*)smem;
   const uint32_t wave_rows = uniform(smem_at + NI * wave * 1024);
-  const int lrow = lane / CPR, key0 = begin + 8 * wave;
-  uint32_t k_chunk[NI], v_chunk;  // the swizzle of V is that of a request's first row in all of them
-#pragma unroll
-  for (int i = 0; i < NI; ++i) k_chunk[i] = (uint32_t)((lane % CPR) ^ F::kswz(8 * wave + i * C::RPI + lrow)) * 16;
-  v_chunk = (uint32_t)((lane % CPR) ^ F::vswz(lrow)) * 16;
+  const int lrow = lane / CPR, key0 = begin + 8 * KG * wave;
+  // chunks of a request's rows in their swizzled places: of K's request i, other by an exclusive or; of V the same in all
+  const uint32_t k_chunk = (uint32_t)((lane % CPR) ^ F::kswz(8 * KG * wave + lrow)) * 16;
+  const uint32_t v_chunk = (uint32_t)((lane % CPR) ^ F::vswz(lrow)) * 16;
   int pages = 0;
   auto look_up = [&](int j) {
     if constexpr (PAGED) {
-      const int key = min(key0 + (j + lane) * BK, src.last);
+      const int key = min(key0 + (j + lane) * BKT, src.last);
       pages = min(max(a.b.table[(long long)it.s * a.b.max_pages + (key >> a.b.page_log2)], 0), a.b.n_pages - 1);
     }
   };
@@ -294,37 +285,30 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
   auto request_rows = [&](const RowsArg& rows, bool is_v, int j, int page, uint32_t slot) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int key = key0 + j * BK + i * C::RPI, lim = max(src.last - key, 0);
-      request(rows.p + src.at(rows, min(key, src.last), page),
-              (uint32_t)min(lrow, lim) * ((uint32_t)rows.rs & 0xFFFFFFu) + (is_v ? v_chunk : k_chunk[i]), wave_rows + slot + i * 1024);
+      const int key = key0 + j * BKT + i * C::RPI, lim = max(src.last - key, 0);
+      const uint32_t chunk = is_v ? v_chunk : k_chunk ^ (uint32_t)(F::kswz(i * C::RPI) * 16);
+      request(rows.p + src.at(rows, min(key, src.last), page), (uint32_t)min(lrow, lim) * ((uint32_t)rows.rs & 0xFFFFFFu) + chunk,
+              wave_rows + slot + i * 1024);
     }
   };
-  // Requests never depend on whether there is a tile to request: past the last one it is requested again, into a slot that
-  // nobody reads any more, and every step has the same number on their way.
+  // Past the last tile that one is requested again, into a slot that nobody reads any more: unmasked steps request without a
+  // branch, and have the same number on their way.
   auto request_k = [&](int j, int page, uint32_t slot) { request_rows(a.k, false, min(j, n_tiles - 1), page, slot); };
-  auto request_v = [&](int j, int page, uint32_t slot) { request_rows(a.v, true, min(j, n_tiles - 1), page, 3 * TILE + slot); };
+  auto request_v = [&](int j, int page, uint32_t slot) { request_rows(a.v, true, min(j, n_tiles - 1), page, NSLOT * TILE + slot); };
 
   // ---- fragments: LDS addresses of the first one in slot 0; the others differ in bits that an exclusive or turns (slots, and the
   // ring, start at multiples of 1 KB).  Made where they are used: kept, they would cost registers that the two sets of scores need.
-  const uint32_t k_at = smem_at + (uint32_t)(rw * ROWB + ((h ^ F::kswz(rw)) * 16));
+  const uint32_t k_at = smem_at + key_g * ROWB + (uint32_t)(rw * ROWB + ((h ^ F::kswz(rw)) * 16));
   uint32_t v_at;
   {
     const int i16 = lane & 15, q2 = (lane >> 4) & 1, vrow = 4 * h + (i16 >> 2);
-    v_at = smem_at + 3 * TILE + (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ F::vswz(vrow)) * 16) + 8 * (i16 & 1));
+    v_at = smem_at + key_g * ROWB + NSLOT * TILE + (uint32_t)(vrow * ROWB + (((2 * q2 + ((i16 & 3) >> 1)) ^ F::vswz(vrow)) * 16) + 8 * (i16 & 1));
   }
   auto kfrags = [&](uint32_t slot, int kb, bf16x8 (&ak)[ND]) {
     uint32_t at = k_at + slot;
     asm volatile("" : "+v"(at));
 #pragma unroll
     for (int dc = 0; dc < ND; ++dc) ak[dc] = *lds_at<bf16x8>((at ^ (dc << 5)) + kb * 32 * ROWB);
-  };
-  auto vfrags = [&](uint32_t at, int g, Frag (&av)[NV]) {
-#pragma unroll
-    for (int dvb = 0; dvb < NV; ++dvb) {
-      const uint32_t vp = (at ^ (dvb << 6)) + g * 16 * ROWB;
-      av[dvb].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp));
-      av[dvb].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp + 8 * ROWB));
-    }
   };
 
   f32x16 o[NV];
@@ -333,7 +317,6 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[i][j] = 0.f;
   float m_ref = -INFINITY, l_run = 0.f;
-  u16x2 most = {0, 0};  // magnitude of V in masked tiles
   const float c2 = a.scale * kLog2e;
 
   auto lift = [&](float mx) {
@@ -356,46 +339,8 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       for (int j = 0; j < 16; ++j) mx = fmaxf(mx, s[kb][j]);
     return max_across_halves(mx) * c2;
   };
-  // LDS reads may not be moved across this point (everything else may): a fragment load stays one group of products ahead of
-  // its use
-  constexpr int kHoldLds = 0x47F;
-  auto weights_pv = [&](f32x16 (&s)[2], uint32_t slot, bool masked) {
-    const float m_use = m_ref == -INFINITY ? 0.f : m_ref;
-    uint32_t vs = v_at + slot;
-    asm volatile("" : "+v"(vs));
-    bf16x8 bp[4];
-    Frag va[2][NV];
-    vfrags(vs, 0, va[0]);  // lands while the weights are computed
-    __builtin_amdgcn_sched_barrier(kHoldLds);
-    float psum = 0.f;
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[g >> 1][8 * (g & 1) + e], c2, -m_use));
-        psum += p;
-        bp[g][e] = (__bf16)p;
-      }
-    l_run += psum;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      if (g + 1 < 4) {
-        vfrags(vs, g + 1, va[(g + 1) & 1]);
-        __builtin_amdgcn_sched_barrier(kHoldLds);
-      }
-      if (masked) {
-#pragma unroll
-        for (int dvb = 0; dvb < NV; ++dvb)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) most = larger_magnitude(most, va[g & 1][dvb].u[e]);
-      }
-#pragma unroll
-      for (int dvb = 0; dvb < NV; ++dvb)
-        o[dvb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[g & 1][dvb].b, bp[g], o[dvb], 0, 0, 0);
-    }
-  };
   auto mask = [&](int tile, f32x16 (&s)[2]) {
-    int n_ok = key_end - begin - tile * BK - 4 * h;  // keys of the tile that count, less the lane's first: made here
+    int n_ok = key_end - tile * BKT - 4 * h;  // keys of the tile that count, less the lane's first: made here
     asm volatile("" : "+v"(n_ok));
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
@@ -415,52 +360,78 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     for (int dc = 0; dc < ND; ++dc) s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak1[dc], bq[dc], s[1], 0, 0, 0);
   };
 
+  // K(0) and the query rows together, the other tiles when they are here: the wait for the rows, which are loaded into
+  // registers, would be one for every request ahead of their use.
+  int page_k = 0, page_v = 0;
   if (n_tiles > 0) {
     look_up(0);
-    int page_k = page_of(0), page_v;
+    page_k = page_of(0);
     request_k(0, page_k, 0);
-    request_v(0, page_k, 0);
-    page_k = page_of(min(1, n_tiles - 1));
-    request_k(1, page_k, TILE);
-    request_v(1, page_k, TILE);
-    page_k = page_of(min(2, n_tiles - 1));
-    request_k(2, page_k, 2 * TILE);
-    wait_loads<4 * NI>();  // K(0) for the first scores
+  }
+  const int r = min(r0 + rw, n_rows - 1);
+  key_end = min(slots_seen(r), end) - begin - key_g;
+  {
+    const char* qp = a.q.p + (kvh * group + r % group) * a.q.hs + (long long)(it.q.first + r / group) * a.q.rs + h * 16;
+#pragma unroll
+    for (int dc = 0; dc < ND; ++dc) bq[dc] = *reinterpret_cast<const bf16x8*>(qp + dc * 32);
+  }
+
+#pragma unroll
+  for (int dc = 0; dc < ND; ++dc) asm volatile("" : "+v"(bq[dc]));
+
+  if (n_tiles > 0) {
+    wait_loads<0>();
     __builtin_amdgcn_s_barrier();
+    request_v(0, page_k, 0);
+    if (n_tiles > 1) {
+      page_k = page_of(1);
+      request_k(1, page_k, TILE);
+    }
+    if (NSLOT == 3 && n_tiles > 1) request_v(1, page_k, TILE);
+    if (NSLOT == 3 && n_tiles > 2) {
+      page_k = page_of(2);
+      request_k(2, page_k, 2 * TILE);
+    }
     f32x16 sA[2], sB[2];
     scores(0, sA);
     // V(0) and K(1) for step 0; K(0) has been read by every wave before step 0 requests its slot's next tile
-    wait_loads<2 * NI>();
+    if (NSLOT == 3 && n_tiles > 2) wait_loads<2 * NI>();
+    else if (NSLOT == 3 && n_tiles > 1) wait_loads<NI>();
+    else wait_loads<0>();
     wait_lds();
     __builtin_amdgcn_s_barrier();
 
-    // Every wave walks all tiles: it requests its rows and meets the barriers, whatever it computes.  Step t requests K(t + 3)
-    // into the slot of K(t), which step t - 1 has read, and V(t + 2) into that of V(t - 1).
+    // Every wave walks all tiles: it requests its rows and meets the barriers, whatever it computes.  Step t requests K(t + NSLOT)
+    // into the slot of K(t), which step t - 1 has read, and V(t + NSLOT - 1) into that of V(t - 1).
     int tile = 0;
-    uint32_t s0 = 0, s1 = TILE, s2 = 2 * TILE;  // slots of tiles t, t + 1, t + 2
+    uint32_t s0 = 0, s1 = TILE, s2 = 2 * TILE;  // slots of tiles t, t + 1 and, of three, t + 2
     auto ahead_k = [&]() {
+      const int j = tile + NSLOT;
       page_v = page_k;
-      if (PAGED && ((tile + 3) & 63) == 0 && tile + 3 < n_tiles) look_up(tile + 3);
-      page_k = page_of(min(tile + 3, n_tiles - 1));
-      request_k(tile + 3, page_k, s0);
+      if (PAGED && (j & 63) == 0 && j < n_tiles) look_up(j);
+      page_k = page_of(min(j, n_tiles - 1));
+      request_k(j, page_k, s0);
     };
-    auto ahead_v = [&]() { request_v(tile + 2, page_v, s2); };
-    auto done = [&]() {  // the next step's tiles were requested one step ago: all but this step's requests have to land
-      wait_loads<2 * NI>();
+    auto ahead_v = [&]() { request_v(tile + NSLOT - 1, page_v, NSLOT == 3 ? s2 : s1); };
+    auto next = [&]() {  // all that the next step reads has landed: of three slots it was requested one step ago
       wait_lds();
       __builtin_amdgcn_s_barrier();
       const uint32_t s = s0;
       s0 = s1;
-      s1 = s2;
-      s2 = s;
+      if constexpr (NSLOT == 3) {
+        s1 = s2;
+        s2 = s;
+      } else {
+        s1 = s;
+      }
       ++tile;
     };
-    // Unmasked tiles, two at a time: S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The
+    // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The
     // order of the instructions is fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier):
     // a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
     // use, and the maximum of the new scores under the last products.
     float mx = 0.f;
-    auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2]) {
+    auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], bool masked) {
       constexpr int NS = 2 * ND, NP = 4 * NV;  // products of S and of O
       uint32_t ks = k_at + s1, vs = v_at + s0;
       asm volatile("" : "+v"(ks), "+v"(vs));
@@ -501,11 +472,11 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         if (i < ND) k_read(i + ND);
         else if (i - ND < 2 * NV) v_read(i - ND);
         if ((i + 1) * 8 / NS > i * 8 / NS) pair(4 + i * 8 / NS);
-        if (i == NS / 4) ahead_k();
-        if (i == NS / 2) ahead_v();
+        if (i == NS / 4 && !masked) ahead_k();
+        if (i == NS / 2 && !masked) ahead_v();
         __builtin_amdgcn_sched_barrier(0);
       }
-      float top = -INFINITY;
+      float top = -INFINITY;  // of the new scores
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         o[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j % (2 * NV)].b, bp[j / NV], o[j % NV], 0, 0, 0);
@@ -525,59 +496,101 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         __builtin_amdgcn_sched_barrier(0);
       }
       l_run += psum;
-      mx = max_across_halves(top) * c2;
-      done();
+      if (!masked) {
+        mx = max_across_halves(top) * c2;
+        wait_loads<C::AHEAD>();
+        next();
+      }
     };
     if (n_full > 1) mx = row_max(sA);
     while (tile + 1 < n_full) {
-      step(sA, sB);
-      step(sB, sA);
+      step(sA, sB, false);
+      step(sB, sA, false);
     }
-    // the masked ones behind them, and an odd unmasked one
-    while (tile < n_any) {
-      ahead_k();
-      ahead_v();
-      mask(tile, sA);
-      lift(row_max(sA));
-      weights_pv(sA, s0, true);
-      if (tile + 1 < n_any) scores(s1, sA);
-      done();
-    }
+    // the masked ones behind them, and an odd unmasked one; then the other waves' tiles
     while (tile < n_tiles) {
-      ahead_k();
-      ahead_v();
-      done();
+      const bool more_k = tile + NSLOT < n_tiles, more_v = tile + NSLOT - 1 < n_tiles;
+      if (more_k) ahead_k();
+      else page_v = page_k;
+      if (more_v) ahead_v();
+      if (tile < n_any) {
+        mask(tile, sA);
+        mx = row_max(sA);
+        step(sA, sB, true);
+        sA[0] = sB[0];
+        sA[1] = sB[1];
+      }
+      if (NSLOT == 3 && more_k) wait_loads<2 * NI>();
+      else if (NSLOT == 3 && more_v) wait_loads<NI>();
+      else wait_loads<0>();
+      next();
     }
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();  // the ring is free for the output rows once nobody's requests are on their way
   }
 
+  if constexpr (KG == 2) {
+    // the second key group hands its running maximum, row sum and outputs to the first (element e of lane l at word e * 64 + l),
+    // which takes both to the common maximum
+    float* mg = reinterpret_cast<float*>(smem + rg * C::MERGE) + lane;
+    if (key_g > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mg[(i * 16 + j) * 64] = o[i][j];
+      mg[NV * 16 * 64] = m_ref;
+      mg[(NV * 16 + 1) * 64] = l_run;
+    }
+    __syncthreads();
+    if (key_g > 0) return;
+    const float m1 = mg[NV * 16 * 64], l1 = mg[(NV * 16 + 1) * 64];
+    const float m_new = fmaxf(m_ref, m1), m_use = m_new == -INFINITY ? 0.f : m_new;
+    const float a0 = __builtin_amdgcn_exp2f(m_ref - m_use), a1 = __builtin_amdgcn_exp2f(m1 - m_use);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[i][j] = o[i][j] * a0 + mg[(i * 16 + j) * 64] * a1;
+    l_run = l_run * a0 + l1 * a1;
+    m_ref = m_new;
+  }
   if (!has_rows) return;
   int rw_end = lane & 31;
   asm volatile("" : "+v"(rw_end));  // the row again: kept, it would cost registers
   const int n_valid = min(32, n_rows - r0);
-  if (__any(most[0] >= 0x7F80 || most[1] >= 0x7F80)) {
-    for (int row = 0; row < n_valid; ++row) attend_row<true, D, PAGED>(a, it, src, r0 + row, begin, wave * 32 + row);
-    return;
-  }
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) sum += fabsf(o[i][j]);
+  const unsigned long long odd2 = __ballot(!(sum < INFINITY));
+  uint32_t odd = (uint32_t)odd2 | (uint32_t)(odd2 >> 32);  // rows whose outputs are not all finite
+  odd &= n_valid < 32 ? (1u << n_valid) - 1 : ~0u;
   const float l_tot = sum_across_halves(l_run), inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
   const float lse2 = m_ref + __log2f(l_tot);
-  char* turn = smem + wave * (C::LDS_BYTES / 8);  // of this wave alone: the ring is free since the last barrier
+  auto again = [&]() {  // behind the wave's own stores
+    for (; odd != 0; odd &= odd - 1) {
+      const int row = __ffs(odd) - 1;
+      attend_row<true, D, PAGED>(a, it, src, r0 + row, begin, rg * 32 + row);
+    }
+  };
+  constexpr int TURN = KG == 2 ? C::MERGE : C::LDS_BYTES / 8;
+  char* turn = smem + rg * TURN;  // of this wave alone: the ring is free since the last barrier
   if (it.n_chunks > 1) {
-    const long long at = part_row(a, it, it.chunk, kvh) + wave * 32;
+    const long long at = part_row(a, it, it.chunk, kvh) + rg * 32;
     store_rows_via_lds<D, 2>(o, inv, a.part_o + at * D, n_valid, turn, lane);
-    if (h == 0 && rw < n_valid) a.part_lse[at + rw] = lse2;
+    if (h == 0 && rw_end < n_valid) a.part_lse[at + rw_end] = lse2;
+    again();
     return;
   }
   constexpr int RS = ROWB + 16;
-  static_assert(32 * RS <= C::LDS_BYTES / 8 && 16 * (D * 4 + 16) <= C::LDS_BYTES / 8, "rows are turned in the ring");
+  static_assert(32 * RS <= TURN && 16 * (D * 4 + 16) <= TURN, "rows are turned in the ring");
 #pragma unroll
   for (int dvb = 0; dvb < NV; ++dvb)
 #pragma unroll
     for (int j4 = 0; j4 < 4; ++j4) {
       const bf16x4 y = {(__bf16)(o[dvb][4 * j4] * inv), (__bf16)(o[dvb][4 * j4 + 1] * inv), (__bf16)(o[dvb][4 * j4 + 2] * inv),
                         (__bf16)(o[dvb][4 * j4 + 3] * inv)};
-      *reinterpret_cast<bf16x4*>(turn + rw * RS + (dvb * 32 + 8 * j4 + 4 * h) * 2) = y;
+      *reinterpret_cast<bf16x4*>(turn + rw_end * RS + (dvb * 32 + 8 * j4 + 4 * h) * 2) = y;
     }
   const int r_end = min(r0 + rw_end, n_rows - 1);
   const int head = kvh * group + r_end % group, tok = it.q.first + r_end / group, pos = lane % CPR;
@@ -590,29 +603,33 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     const uint32_t lo = __shfl((uint32_t)to, row), hi = __shfl((uint32_t)((unsigned long long)to >> 32), row);
     if (row < n_valid) *reinterpret_cast<u32x4*>(a.out.p + (long long)((unsigned long long)hi << 32 | lo) + pos * 16) = y;
   }
-  if (h == 0 && rw < n_valid && a.lse != nullptr) a.lse[(long long)head * a.b.n_rows + tok] = lse2 * kLn2;
+  if (h == 0 && rw_end < n_valid && a.lse != nullptr) a.lse[(long long)head * a.b.n_rows + tok] = lse2 * kLn2;
+  again();
 }
 
-// Batches in which some sequences have many rows: 256 at a time for those, 32 shared by the eight waves for the others.
-template <int D, bool PAGED>
+// Batches in which some sequences have many rows: wide tiles for those, 32 rows shared by the eight waves for the others.
+template <int D, bool PAGED, int KG>
 __global__ __launch_bounds__(512, 2) void k_attend_mixed(PagedAttnLaunch a) {
   const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<true, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  const Item it = find_item<KG, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
   if (it.s < 0 || !has_room(a, it)) return;
-  if (it.wide) attend_wide<D, PAGED>(a, it, kvh);
+  if (it.wide) attend_wide<D, PAGED, KG>(a, it, kvh);
   else attend_few<D, PAGED, 8>(a, it, kvh);
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-template <int D>
+constexpr long long kFewTotal = 24576, kMidTotal = 131072;
+
+template <int D, int KG>
 constexpr int mixed_lds() {
-  return WideCfg<D>::LDS_BYTES > FewCfg<D, 8>::LDS_BYTES ? WideCfg<D>::LDS_BYTES : FewCfg<D, 8>::LDS_BYTES;
+  return WideCfg<D, KG>::LDS_BYTES > FewCfg<D, 8>::LDS_BYTES ? WideCfg<D, KG>::LDS_BYTES : FewCfg<D, 8>::LDS_BYTES;
 }
 
 template <int D, bool PAGED>
 hipError_t run_bf16(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
   const dim3 grid((unsigned)(p.max_items * a.hkv));
-  if (p.wide) hipLaunchKernelGGL((k_attend_mixed<D, PAGED>), grid, dim3(512), mixed_lds<D>(), s, a);
+  if (p.kg == 2) hipLaunchKernelGGL((k_attend_mixed<D, PAGED, 2>), grid, dim3(512), (mixed_lds<D, 2>()), s, a);
+  else if (p.kg == 1) hipLaunchKernelGGL((k_attend_mixed<D, PAGED, 1>), grid, dim3(512), (mixed_lds<D, 1>()), s, a);
   else hipLaunchKernelGGL((k_attend_few<D, PAGED>), grid, dim3(256), (FewCfg<D, 4>::LDS_BYTES), s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.joins) return e;
@@ -621,10 +638,10 @@ hipError_t run_bf16(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_
 
 template <int D, bool PAGED>
 hipError_t raise_limit() {
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_few<D, PAGED>),
-                                           hipFuncAttributeMaxDynamicSharedMemorySize, FewCfg<D, 4>::LDS_BYTES);
-  return e != hipSuccess ? e : hipFuncSetAttribute(reinterpret_cast<const void*>(&k_attend_mixed<D, PAGED>),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, mixed_lds<D>());
+  auto raise = [](const void* f, int bytes) { return hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); };
+  hipError_t e = raise(reinterpret_cast<const void*>(&k_attend_few<D, PAGED>), FewCfg<D, 4>::LDS_BYTES);
+  if (e == hipSuccess) e = raise(reinterpret_cast<const void*>(&k_attend_mixed<D, PAGED, 1>), mixed_lds<D, 1>());
+  return e != hipSuccess ? e : raise(reinterpret_cast<const void*>(&k_attend_mixed<D, PAGED, 2>), mixed_lds<D, 2>());
 }
 
 }  // namespace
@@ -633,15 +650,16 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
   auto less = [](long long x, long long y) { return x < y ? x : y; };
-  p.wide = dtype == SAMKV_BF16 && most > kFewRows;
-  p.target = p.wide ? 256 : 512;  // as many workgroups as are resident at once
+  p.kg = dtype != SAMKV_BF16 || most <= kFewRows ? 0 : rows * hkv <= kFewTotal ? 0 : rows * hkv <= kMidTotal ? 2 : 1;
+  p.target = p.kg > 0 ? 256 : 512;  // as many workgroups as are resident at once
   p.min_chunk = 256;
+  const long long wide = p.kg == 2 ? 128 : 256;
   // Prompts that fill the chip many times over are not cut: the join would be one more launch.
-  p.joins = max_len > p.min_chunk && (paged || rows / kWideRows * hkv < 4 * p.target);
-  // Items: the tiles of 32 rows that there can be, or of 256 and those of sequences with few rows, and the chunks that find_item
-  // cuts (a chunk holds at least 1 / target of the cost of all heads, and a tile's cost is at least half of its keys').
-  const long long few_most = p.wide ? kFewRows : most, per = p.wide ? kWideRows / 32 : 1, shares = (p.target + hkv - 1) / hkv;
-  const long long tiles = less(n * ((few_most + 31) / 32), rows / 32 + n) + (p.wide ? less(n * ((most + kWideRows - 1) / kWideRows), rows / kWideRows + n) : 0);
+  p.joins = max_len > p.min_chunk && (paged || rows / (p.kg > 0 ? wide : 32) * hkv < 2 * p.target);
+  // Items: the tiles of 32 rows that there can be, or the wide ones and those of sequences with few rows, and the chunks that
+  // find_item cuts (a chunk holds at least 1 / target of the cost of all heads, and a tile's cost is at least half of its keys').
+  const long long few_most = p.kg > 0 ? kFewRows : most, per = p.kg > 0 ? wide / 32 : 1, shares = (p.target + hkv - 1) / hkv;
+  const long long tiles = less(n * ((few_most + 31) / 32), rows / 32 + n) + (p.kg > 0 ? less(n * ((most + wide - 1) / wide), rows / wide + n) : 0);
   p.max_items = (int)(tiles + (p.joins ? 2 * shares : 0));
   // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
   p.max_slots = (int)(p.joins ? less(p.max_items, 4 * shares) * per : 0);

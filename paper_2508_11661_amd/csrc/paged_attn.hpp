@@ -11,34 +11,41 @@ typedef const __attribute__((address_space(4))) int32_t* ScalarInts;
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-__device__ __forceinline__ int scan64(int x, int lane) {  // inclusive prefix sum over the lanes
-#pragma unroll
-  for (int w = 1; w < 64; w *= 2) {
-    const int y = __shfl_up(x, w);
-    if (lane >= w) x += y;
-  }
+__device__ __forceinline__ int scan64(int x) {  // inclusive prefix sum over the lanes, on the vector ALU
+#define SAMKV_STEP(ctrl, rows) x += __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xF, false)
+  SAMKV_STEP(0x111, 0xF);  // one, two, four and eight lanes up within a row of 16
+  SAMKV_STEP(0x112, 0xF);
+  SAMKV_STEP(0x114, 0xF);
+  SAMKV_STEP(0x118, 0xF);
+  SAMKV_STEP(0x142, 0xA);  // the last lane of a row to the next row, of the first half to the second
+  SAMKV_STEP(0x143, 0xC);
+#undef SAMKV_STEP
   return x;
 }
+__device__ __forceinline__ int last_of(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-// Sequences of at most kFewRows rows per KV head are cut into tiles of 32 rows, the others, where there is a kernel for that
-// (WIDE), into tiles of kWideRows.
-constexpr int kFewRows = 128, kWideRows = 256;
-constexpr int kWideCost = 5;  // time of a wide tile over a number of keys, in tiles of 32 rows
+// Sequences of at most kFewRows rows per KV head are cut into tiles of 32 rows, the others into wide ones where the launch has
+// them: KG = 1, 256 rows, KG = 2, 128 rows whose keys two groups of waves share; KG = 0: no wide tiles.
+constexpr int kFewRows = 128;
+template <int KG>
+constexpr int wide_rows() { return KG == 2 ? 128 : 256; }
+template <int KG>
+constexpr int wide_cost() { return KG == 2 ? 3 : 5; }  // time of a wide tile over a number of keys, in tiles of 32 rows
 
 struct Item {
   int s;                     // sequence; < 0: no item
   bool wide;
+  int slots;                 // of a (tile, chunk) whose result is a part: one per 32 rows
   int tile, chunk, n_chunks, tiles;
   int c;                     // keys of a chunk
   int first_slot;            // slots of partial results ahead of the sequence's
   SeqSpan q;
-  __device__ __forceinline__ int slots() const { return wide ? kWideRows / 32 : 1; }  // of a (tile, chunk) that is a part
 };
 
 // Item number `index`.  JOIN: group of 32 rows number `index` among the tiles whose keys are cut; *rows32 is the group's number in
 // its tile, and the chunk is the first.  Called by whole waves; the result is the same in every lane.  Within a sequence items
 // run chunk by chunk, the last tile (with the most keys) first.
-template <bool WIDE, bool JOIN>
+template <int KG, bool JOIN>
 __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, int index, int lane, int* rows32 = nullptr) {
   const BatchArg& b = a.b;
   auto span = [&](int s) {
@@ -46,9 +53,9 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
     if (s >= b.n_seq) q.n = q.len = 0;
     return q;
   };
-  auto is_wide = [&](const SeqSpan& q) { return WIDE && (long long)q.n * group > kFewRows; };
+  auto is_wide = [&](const SeqSpan& q) { return KG > 0 && (long long)q.n * group > kFewRows; };
   auto n_tiles = [&](const SeqSpan& q) {
-    const int rows = is_wide(q) ? kWideRows : 32;
+    const int rows = is_wide(q) ? wide_rows<KG>() : 32;
     return (int)(((long long)q.n * group + rows - 1) / rows);
   };
   SeqSpan q = span(lane);
@@ -62,14 +69,15 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
     for (int s = lane; s < b.n_seq; s += 64) {
       const SeqSpan x = s == lane ? q : span(s);
       const long long keys = max(x.len - x.n / 2, (x.len + 1) / 2);
-      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * keys * (is_wide(x) ? kWideCost : 1);
+      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * keys * (is_wide(x) ? wide_cost<KG>() : 1);
     }
-#pragma unroll
-    for (int w = 1; w < 64; w *= 2) total += __shfl_xor(total, w);
+    // lane by lane in two halves: sums of 64 numbers below 2^24 and of their upper parts
+    const unsigned long long high = (unsigned)last_of(scan64((int)(total >> 24)));
+    total = (high << 24) + (unsigned)last_of(scan64((int)(total & 0xFFFFFF)));
     const unsigned long long share = (total * a.hkv + a.target - 1) / a.target;
     it.c = uniform((int)min(share, 0x40000000ull));
   }
-  const int c_few = max((it.c + 63) / 64 * 64, a.min_chunk), c_wide = max((it.c / kWideCost + 64) / 64 * 64, 2 * a.min_chunk);
+  const int c_few = max((it.c + 63) / 64 * 64, a.min_chunk), c_wide = max((it.c / wide_cost<KG>() + 128) / 128 * 128, 2 * a.min_chunk);
   it.s = -1;
   int before = 0, slots_before = 0;
   for (int s0 = 0; s0 < b.n_seq; s0 += 64) {
@@ -77,14 +85,14 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
       q = span(s0 + lane);
       tiles = n_tiles(q);
     }
-    const int c = is_wide(q) ? c_wide : c_few, per = is_wide(q) ? kWideRows / 32 : 1;
+    const int c = is_wide(q) ? c_wide : c_few, per = is_wide(q) ? wide_rows<KG>() / 32 : 1;
     const int chunks = max((q.len + c - 1) / c, 1), items = tiles * chunks, slots = chunks > 1 ? items * per : 0;
     const int count = JOIN ? (chunks > 1 ? tiles * per : 0) : items;
-    const int upto = scan64(count, lane) + before, slots_to = scan64(slots, lane) + slots_before;
+    const int upto = scan64(count) + before, slots_to = a.max_chunks > 1 ? scan64(slots) + slots_before : 0;
     const unsigned long long past = __ballot(upto > index);
     if (past != 0) {
       const int at = __ffsll(past) - 1;
-      auto of = [&](int x) { return uniform(__shfl(x, at)); };
+      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
       it.s = s0 + at;
       it.tiles = of(tiles);
       it.n_chunks = of(chunks);
@@ -94,19 +102,21 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
       it.q.len = of(q.len);
       it.wide = is_wide(it.q);
       it.c = it.wide ? c_wide : c_few;
+      it.slots = it.wide ? wide_rows<KG>() / 32 : 1;
       const int local = index - of(upto - count);
       if constexpr (JOIN) {
         it.chunk = 0;
-        it.tile = local / it.slots();
-        *rows32 = local % it.slots();
+        it.tile = local / it.slots;
+        *rows32 = local % it.slots;
       } else {
         it.chunk = local / it.tiles;
         it.tile = it.tiles - 1 - local % it.tiles;
       }
+      if (local < 0 || it.chunk >= it.n_chunks || it.tile >= it.tiles) it.s = -1;  // counts that have overflowed: see has_room
       return it;
     }
-    before = uniform(__shfl(upto, 63));
-    slots_before = uniform(__shfl(slots_to, 63));
+    before = last_of(upto);
+    slots_before = last_of(slots_to);
   }
   return it;
 }
@@ -114,14 +124,14 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
 // First slot of a (tile, chunk)'s partial result (one of every KV head stands there), and the row of part_lse and part_o that
 // one head's begins at.
 __device__ __forceinline__ int part_slot(const Item& it, int chunk) {
-  return it.first_slot + (chunk * it.tiles + it.tiles - 1 - it.tile) * it.slots();
+  return it.first_slot + (chunk * it.tiles + it.tiles - 1 - it.tile) * it.slots;
 }
 __device__ __forceinline__ long long part_row(const PagedAttnLaunch& a, const Item& it, int chunk, int kvh) {
-  return ((long long)part_slot(it, chunk) * a.hkv + (long long)kvh * it.slots()) * a.tile_rows;
+  return ((long long)part_slot(it, chunk) * a.hkv + (long long)kvh * it.slots) * a.tile_rows;
 }
 // Prefix sums that go backwards can ask for more room than the batch's rows do; what has none is left out.
 __device__ __forceinline__ bool has_room(const PagedAttnLaunch& a, const Item& it) {
-  return it.n_chunks == 1 || part_slot(it, it.n_chunks - 1) + it.slots() <= a.max_slots;
+  return it.n_chunks == 1 || (part_slot(it, 0) >= 0 && part_slot(it, it.n_chunks - 1) + it.slots <= a.max_slots);
 }
 
 // Where the keys and values of a sequence's KV head lie.
@@ -142,9 +152,10 @@ struct KvSource {
   }
 };
 
-// One row of a sequence against the keys of its item's chunk by a wave, key by key: what a workgroup falls back on that has met
-// an infinity or a NaN among its values.  The matrix products multiply the values of keys that a row does not see by zero, and
-// two-term weights have terms of zero and of either sign; here a value meets the weight of a row that sees it, and nothing else.
+// One row of a sequence against the keys of its item's chunk by a wave, key by key, so that a value meets the weight of a row that
+// sees it and nothing else.  The matrix products multiply the values of keys that a row does not see by zero, and two-term weights
+// have terms of zero and of either sign: infinities and NaN among the values make NaN of the outputs of any row.  Rows whose outputs
+// are not all finite are therefore computed once more like this.
 template <bool BF16, int D, bool PAGED>
 __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item& it, const KvSource<PAGED>& src, int r, int begin, int row) {
   constexpr int CPL = D / 64;
@@ -201,35 +212,25 @@ __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item&
 }
 
 // Joins the partial results of NW waves over one tile of 32 rows and writes them (as the item's, or as a part of them): maxima
-// and sums first, then the rows, each wave's scaled to the common maximum, through LDS.  `bad`: the wave has met an infinity or a
-// NaN among its values.
+// and sums first, then the rows, each wave's scaled to the common maximum, through LDS.
 constexpr int join_area(int d) { return 32 * (d * 4 + 16); }  // LDS bytes of a wave's rows (pad: 16 rows hit 64 distinct banks)
-constexpr int join_lds(int nw, int area) { return nw * area + nw * (32 * 8 + 4); }
+constexpr int join_lds(int nw, int area) { return nw * area + nw * 32 * 8; }
 template <int D, int NW, bool BF16, bool PAGED, int AREA>
 __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item& it, const KvSource<PAGED>& src, f32x16 (&o)[D / 32],
-                                           float m_run, float l_run, bool bad, int begin) {
+                                           float m_run, float l_run, int begin) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   constexpr int NV = D / 32, OROW = D * 4 + 16;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), rw = lane & 31, h = lane >> 5;
   const int group = a.hq / a.hkv, kvh = src.kvh, n_rows = it.q.n * group, r0 = it.tile * 32;
   float* s_m = reinterpret_cast<float*>(smem + NW * AREA);
   float* s_l = s_m + NW * 32;
-  int* s_bad = reinterpret_cast<int*>(s_l + NW * 32);
   const float l_row = sum_across_halves(l_run);
   if (h == 0) {
     s_m[wave * 32 + rw] = m_run;
     s_l[wave * 32 + rw] = l_row;
   }
-  if (lane == 0) s_bad[wave] = bad;
   __syncthreads();
   const int n_valid = min(32, n_rows - r0);
-  bool any_bad = false;
-#pragma unroll
-  for (int w = 0; w < NW; ++w) any_bad |= s_bad[w] != 0;
-  if (any_bad) {
-    for (int row = wave; row < n_valid; row += NW) attend_row<BF16, D, PAGED>(a, it, src, r0 + row, begin, row);
-    return;
-  }
   auto joined = [&](int row, float* m_out) {
     float m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -258,9 +259,9 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
     }
   }
   __syncthreads();
-  constexpr int LPR = D / 4;
-  for (int row = threadIdx.x / LPR; row < n_valid; row += NW * 64 / LPR) {
-    const int c4 = threadIdx.x % LPR;
+  constexpr int LPR = D / 4, RPW = 64 / LPR;  // lanes per row, rows of a wave at a time
+  for (int row0 = wave * RPW; row0 < n_valid; row0 += NW * RPW) {
+    const int row = min(row0 + lane / LPR, n_valid - 1), c4 = lane % LPR;
     f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -268,6 +269,15 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
+    const unsigned long long odd = __ballot(!(fabsf(x[0]) + fabsf(x[1]) + fabsf(x[2]) + fabsf(x[3]) < INFINITY));
+    if (odd != 0) {
+#pragma unroll 1
+      for (int i = 0; i < RPW && row0 + i < n_valid; ++i)
+        if ((odd >> (i * LPR) & ((1ull << LPR) - 1)) != 0)
+          attend_row<BF16, D, PAGED>(a, it, src, r0 + row0 + i, begin, row0 + i);
+      if (row0 + lane / LPR >= n_valid || (odd >> (lane / LPR * LPR) & ((1ull << LPR) - 1)) != 0) continue;
+    }
+    if (row0 + lane / LPR >= n_valid) continue;
     float m;
     const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -293,15 +303,15 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
 
 // out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
 // four channels a lane).
-template <int D, bool BF16, bool WIDE>
+template <int D, bool BF16, int KG>
 __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
   constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
   const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
   const int kvh = blockIdx.x % a.hkv;
   int rows32 = 0;
-  const Item it = find_item<WIDE, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
+  const Item it = find_item<KG, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
   if (it.s < 0 || !has_room(a, it)) return;
-  const int tile0 = it.tile * 32 * it.slots(), n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
+  const int tile0 = it.tile * 32 * it.slots, n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
   for (int row = rows32 * 32 + uniform(blockIdx.y * 4 + (threadIdx.x >> 6)); row < n_rows; row += 4 * gridDim.y) {
     const int rr = tile0 + row;
     const int c4 = lane % LPR, cg = lane / LPR;
@@ -364,9 +374,10 @@ __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
 template <int D, bool BF16>
 hipError_t launch_join(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
   // a tile that is cut has two slots at least
-  const dim3 grid((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.wide ? 1 : (p.tile_rows + 3) / 4));
-  if (p.wide) hipLaunchKernelGGL((k_join_chunks<D, BF16, true>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_join_chunks<D, BF16, false>), grid, dim3(256), 0, s, a);
+  const dim3 grid((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.kg > 0 ? 1 : (p.tile_rows + 3) / 4));
+  if (p.kg == 2) hipLaunchKernelGGL((k_join_chunks<D, BF16, 2>), grid, dim3(256), 0, s, a);
+  else if (p.kg == 1) hipLaunchKernelGGL((k_join_chunks<D, BF16, 1>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_join_chunks<D, BF16, 0>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

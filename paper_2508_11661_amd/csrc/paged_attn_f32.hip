@@ -53,7 +53,7 @@ __device__ __forceinline__ void attend_f32(const PagedAttnLaunch& a, const Item&
   for (int b = 0; b < NV; ++b)
 #pragma unroll
     for (int j = 0; j < 16; ++j) o[b][j] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f, odd = 0.f;  // odd: 0, or NaN once a value was infinite or NaN
+  float m_run = -INFINITY, l_run = 0.f;
   const float c2 = (float)((double)a.scale * 1.4426950408889634074);
 
   int k0 = begin + wave * 32;
@@ -118,9 +118,7 @@ __device__ __forceinline__ void attend_f32(const PagedAttnLaunch& a, const Item&
     for (int j = 0; j < 16; ++j) {
 #pragma unroll
       for (int b = 0; b < NV; ++b) {
-        const float v = vx[(j * NV + b) % NVX];
-        odd = fmaf(v, 0.f, odd);
-        o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[j], o[b], 0, 0, 0);
+        o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(vx[(j * NV + b) % NVX], s[j], o[b], 0, 0, 0);
       }
       if ((j + 1) * NV + NVX <= 16 * NV) {
 #pragma unroll
@@ -134,13 +132,13 @@ __device__ __forceinline__ void attend_f32(const PagedAttnLaunch& a, const Item&
     }
     x = next;
   }
-  join_waves<D, NW, false, PAGED, join_area(D)>(a, it, src, o, m_run, l_run, __any(odd != 0.f), begin);
+  join_waves<D, NW, false, PAGED, join_area(D)>(a, it, src, o, m_run, l_run, begin);
 }
 
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * NW, 2) void k_attend_f32(PagedAttnLaunch a) {
   const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<false, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
+  const Item it = find_item<0, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
   if (it.s < 0 || !has_room(a, it)) return;
   attend_f32<D, PAGED>(a, it, kvh);
 }
