@@ -238,6 +238,11 @@ struct WideCfg {
   static_assert(NI * RPI == 8 * KG, "rows of a wave");
 };
 
+template <bool M>
+struct Masked {
+  static constexpr bool value = M;
+};
+
 template <int D, bool PAGED, int KG>
 __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item& it, int kvh) {
   using C = WideCfg<D, KG>;
@@ -323,11 +328,13 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     if (__any(mx > m_ref + TAU)) {
       const float m_new = fmaxf(m_ref, mx);
       const float al = __builtin_amdgcn_exp2f(m_ref - (m_new == -INFINITY ? 0.f : m_new));
-      l_run *= al;
+      if (__any(m_ref != -INFINITY)) {  // not the first tile
+        l_run *= al;
 #pragma unroll
-      for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[i][j] *= al;
+          for (int j = 0; j < 16; ++j) o[i][j] *= al;
+      }
       m_ref = m_new;
     }
   };
@@ -426,12 +433,12 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       }
       ++tile;
     };
-    // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The
-    // order of the instructions is fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier):
+    // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The order of the instructions is fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier):
     // a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
     // use, and the maximum of the new scores under the last products.
     float mx = 0.f;
-    auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], bool masked) {
+    auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto kind) {
+      constexpr bool masked = kind.value;
       constexpr int NS = 2 * ND, NP = 4 * NV;  // products of S and of O
       uint32_t ks = k_at + s1, vs = v_at + s0;
       asm volatile("" : "+v"(ks), "+v"(vs));
@@ -485,7 +492,7 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         if (j < EARLY) {
 #pragma unroll
           for (int k = 0; k < PER; ++k) pair(12 + j * PER + k);
-        } else {
+        } else if constexpr (!masked) {
 #pragma unroll
           for (int k = 0; k < MAXES; ++k) {
             const int v = (j - EARLY) * MAXES + k;
@@ -496,7 +503,7 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         __builtin_amdgcn_sched_barrier(0);
       }
       l_run += psum;
-      if (!masked) {
+      if constexpr (!masked) {
         mx = max_across_halves(top) * c2;
         wait_loads<C::AHEAD>();
         next();
@@ -504,8 +511,8 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     };
     if (n_full > 1) mx = row_max(sA);
     while (tile + 1 < n_full) {
-      step(sA, sB, false);
-      step(sB, sA, false);
+      step(sA, sB, Masked<false>{});
+      step(sB, sA, Masked<false>{});
     }
     // the masked ones behind them, and an odd unmasked one; then the other waves' tiles
     while (tile < n_tiles) {
@@ -516,7 +523,7 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       if (tile < n_any) {
         mask(tile, sA);
         mx = row_max(sA);
-        step(sA, sB, true);
+        step(sA, sB, Masked<true>{});
         sA[0] = sB[0];
         sA[1] = sB[1];
       }
@@ -618,8 +625,6 @@ __global__ __launch_bounds__(512, 2) void k_attend_mixed(PagedAttnLaunch a) {
 }
 
 // ---------------------------------------------------------------------------------------------- launches
-constexpr long long kFewTotal = 24576, kMidTotal = 131072;
-
 template <int D, int KG>
 constexpr int mixed_lds() {
   return WideCfg<D, KG>::LDS_BYTES > FewCfg<D, 8>::LDS_BYTES ? WideCfg<D, KG>::LDS_BYTES : FewCfg<D, 8>::LDS_BYTES;
@@ -646,23 +651,43 @@ hipError_t raise_limit() {
 
 }  // namespace
 
+// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2 us, 1.4 where the chip is not full),
+// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each, one and a half for
+// tiles of 32 rows, of which two share one.
+// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, tiles of 32 / 128 / 256
+// rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 11 / 13 / 14, 1 x 1000 34 / 25 / 34, 1 x 2048 90 / 52 / 63, 1 x 4096 311 / 175 /
+// 157, 4 x 512 48 / 33 / 26, 32 x 64 30 / 22 / 15, 20 x 300 97 / 71 / 48; d = 64, 8 heads: 1 x 700 11 / 14 / 18, 1 x 2048 19 / 25 /
+// 38, 1 x 4096 50 / 42 / 68.
+static int prompt_shape(long long rows, long long mean_len, int max_len) {
+  const double longest = max_len / 64.0, mean = mean_len / 128.0;
+  auto time = [&](double tile, double resident, double of_longest, double of_mean, double ends) {
+    const double a = of_longest * longest + ends, b = rows / tile / resident * (of_mean * mean + ends);
+    return a > b ? a : b;
+  };
+  const double few = time(32, 512, 0.45, 0.7, 1.5), mid = time(128, 256, 0.5, 0.5, 4), wide = time(256, 256, 1, 1, 4);
+  return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
+}
+// New tokens over a cache, whose keys are cut into chunks until the chip is full: tiles of 32 rows where no sequence has more than
+// three of them (a wide tile costs about that), 128 where there are few rows (4 x 256 tokens over 3000, 32 heads: 115 / 62 / 78;
+// 2 x 512 over 8000: 264 / 138 / 153; 1 x 2048 over 16000: 953 / 508 / 486).
+static int paged_shape(long long most, long long rows) { return most <= 96 ? 0 : rows <= 49152 ? 2 : 1; }
+
 PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
   auto less = [](long long x, long long y) { return x < y ? x : y; };
-  p.kg = dtype != SAMKV_BF16 || most <= kFewRows ? 0 : rows * hkv <= kFewTotal ? 0 : rows * hkv <= kMidTotal ? 2 : 1;
+  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv) : prompt_shape(rows * hkv, n_rows / n, max_len);
   p.target = p.kg > 0 ? 256 : 512;  // as many workgroups as are resident at once
   p.min_chunk = 256;
   const long long wide = p.kg == 2 ? 128 : 256;
-  // Prompts that fill the chip many times over are not cut: the join would be one more launch.
-  p.joins = max_len > p.min_chunk && (paged || rows / (p.kg > 0 ? wide : 32) * hkv < 2 * p.target);
-  // Items: the tiles of 32 rows that there can be, or the wide ones and those of sequences with few rows, and the chunks that
-  // find_item cuts (a chunk holds at least 1 / target of the cost of all heads, and a tile's cost is at least half of its keys').
-  const long long few_most = p.kg > 0 ? kFewRows : most, per = p.kg > 0 ? wide / 32 : 1, shares = (p.target + hkv - 1) / hkv;
-  const long long tiles = less(n * ((few_most + 31) / 32), rows / 32 + n) + (p.kg > 0 ? less(n * ((most + wide - 1) / wide), rows / wide + n) : 0);
-  p.max_items = (int)(tiles + (p.joins ? 2 * shares : 0));
+  p.joins = paged && max_len > p.min_chunk;  // prompts have rows enough: the join would be one more launch
+  // Items: the tiles that there can be, and the chunks that find_item cuts (one holds at least 1 / target of the keys that the
+  // tiles of all heads see).
+  const long long tile = p.kg > 0 ? wide : 32, shares = (p.target + hkv - 1) / hkv;
+  const long long tiles = less(n * ((most + tile - 1) / tile), rows / tile + n);
+  p.max_items = (int)(tiles + (p.joins ? shares : 0));
   // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
-  p.max_slots = (int)(p.joins ? less(p.max_items, 4 * shares) * per : 0);
+  p.max_slots = (int)(p.joins ? less(p.max_items, 2 * shares) * (tile / 32) : 0);
   p.tile_rows = (int)less(32, most);
   const size_t part_rows = (size_t)p.max_slots * hkv * p.tile_rows;
   p.part_lse = (part_rows * d * 4 + 255) / 256 * 256;

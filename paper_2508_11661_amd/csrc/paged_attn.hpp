@@ -24,9 +24,10 @@ __device__ __forceinline__ int scan64(int x) {  // inclusive prefix sum over the
 }
 __device__ __forceinline__ int last_of(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-// Sequences of at most kFewRows rows per KV head are cut into tiles of 32 rows, the others into wide ones where the launch has
-// them: KG = 1, 256 rows, KG = 2, 128 rows whose keys two groups of waves share; KG = 0: no wide tiles.
-constexpr int kFewRows = 128;
+// Tiles have 32 rows (KG = 0); or, in launches that have wide ones, sequences of at most 32 rows per KV head are one tile of 32 and
+// the others are cut into wide tiles: KG = 1, 256 rows, KG = 2, 128 rows whose keys two groups of waves share.  So there are no
+// more items than whole tiles in the batch's rows and sequences, and the grid has few workgroups without an item.
+constexpr int kFewRows = 32;
 template <int KG>
 constexpr int wide_rows() { return KG == 2 ? 128 : 256; }
 template <int KG>
@@ -64,12 +65,11 @@ __device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, i
   it.c = 0x40000000;
   if (a.max_chunks > 1) {
     // keys of a chunk of 32 rows: the cost of all tiles and heads over the number of workgroups; a wide tile's are fewer by
-    // what it costs more.  A tile of new tokens sees on average half of them, and at least half of len.
+    // what it costs more.
     unsigned long long total = 0;
     for (int s = lane; s < b.n_seq; s += 64) {
       const SeqSpan x = s == lane ? q : span(s);
-      const long long keys = max(x.len - x.n / 2, (x.len + 1) / 2);
-      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * keys * (is_wide(x) ? wide_cost<KG>() : 1);
+      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * x.len * (is_wide(x) ? wide_cost<KG>() : 1);
     }
     // lane by lane in two halves: sums of 64 numbers below 2^24 and of their upper parts
     const unsigned long long high = (unsigned)last_of(scan64((int)(total >> 24)));
