@@ -63,7 +63,7 @@ hipError_t launch_paged_append(const AppendLaunch& a, hipStream_t s);
 // token by token (row t G + g), cut into tiles; the keys that a tile sees are cut into chunks of `chunk` keys, whose partial
 // results a second kernel joins.  A work item is (sequence, tile, chunk), a workgroup one item of one KV head.  The grid has
 // room for every batch within the host's bounds; which item a workgroup takes, and how long a chunk is, every wave finds from
-// the lengths (find_item): the keys of all tiles are shared out over as many workgroups as are wanted (`target`), so that a
+// the lengths (Items): the keys of all tiles are shared out over as many workgroups as are wanted, so that a
 // long sequence among short ones does not hold up the batch.
 struct PagedAttnLaunch {
   int dtype, d, hq, hkv, paged;
@@ -72,7 +72,7 @@ struct PagedAttnLaunch {
   RowsArg k, v;  // pages: hs = bytes of one head's rows of a page, rs = bytes of a row
   float* lse;    // may be null
   float scale;
-  int target, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys (wide tiles: twice that)
+  int target_log2, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys (wide tiles: twice that)
   int max_chunks;         // 1: no sequence's keys are cut
   // partial results of the tiles whose keys are cut, in slots of 32 rows (of tile_rows, where no tile has more)
   int max_slots, tile_rows;
@@ -83,8 +83,9 @@ hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
 
 // Sizes of a launch that follow from the bounds alone.
 struct PagedAttnPlan {
-  int kg;  // which wide tiles there are: see paged_attn.hpp
-  int target, min_chunk, max_items, max_slots, tile_rows;
+  int kg;     // which wide tiles there are: see paged_attn.hpp
+  bool once;  // every sequence is one tile of 32 rows
+  int target_log2, min_chunk, max_items, max_slots, tile_rows;
   bool joins;  // whether any sequence can have more than one chunk
   size_t part_lse, bytes;  // workspace: part_o, then part_lse
 };

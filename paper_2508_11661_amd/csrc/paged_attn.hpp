@@ -43,83 +43,129 @@ struct Item {
   SeqSpan q;
 };
 
-// Item number `index`.  JOIN: group of 32 rows number `index` among the tiles whose keys are cut; *rows32 is the group's number in
-// its tile, and the chunk is the first.  Called by whole waves; the result is the same in every lane.  Within a sequence items
-// run chunk by chunk, the last tile (with the most keys) first.
+// Finds work items: JOIN = false, number `index` of them; JOIN = true, group of 32 rows number `index` among the tiles whose keys
+// are cut (the chunk is the first).  All calls are by whole waves, and the results are the same in every lane.  A lane holds one
+// of 64 sequences; batches of up to that many are read once, and their wide tiles taken in order of falling length, so that a long
+// sequence's are not the last to start.  Within a sequence items run chunk by chunk, the last tile (with the most keys) first.
 template <int KG, bool JOIN>
-__device__ __forceinline__ Item find_item(const PagedAttnLaunch& a, int group, int index, int lane, int* rows32 = nullptr) {
-  const BatchArg& b = a.b;
-  auto span = [&](int s) {
-    SeqSpan q = seq_span(b, min(s, b.n_seq - 1));
-    if (s >= b.n_seq) q.n = q.len = 0;
-    return q;
-  };
-  auto is_wide = [&](const SeqSpan& q) { return KG > 0 && (long long)q.n * group > kFewRows; };
-  auto n_tiles = [&](const SeqSpan& q) {
-    const int rows = is_wide(q) ? wide_rows<KG>() : 32;
-    return (int)(((long long)q.n * group + rows - 1) / rows);
-  };
-  SeqSpan q = span(lane);
-  int tiles = n_tiles(q);
-  Item it;
-  it.c = 0x40000000;
-  if (a.max_chunks > 1) {
-    // keys of a chunk of 32 rows: the cost of all tiles and heads over the number of workgroups; a wide tile's are fewer by
-    // what it costs more.
-    unsigned long long total = 0;
-    for (int s = lane; s < b.n_seq; s += 64) {
-      const SeqSpan x = s == lane ? q : span(s);
-      total += (unsigned long long)(s == lane ? tiles : n_tiles(x)) * x.len * (is_wide(x) ? wide_cost<KG>() : 1);
-    }
-    // lane by lane in two halves: sums of 64 numbers below 2^24 and of their upper parts
-    const unsigned long long high = (unsigned)last_of(scan64((int)(total >> 24)));
-    total = (high << 24) + (unsigned)last_of(scan64((int)(total & 0xFFFFFF)));
-    const unsigned long long share = (total * a.hkv + a.target - 1) / a.target;
-    it.c = uniform((int)min(share, 0x40000000ull));
+struct Items {
+  const PagedAttnLaunch& a;
+  const int lane, group;
+  int c_few, c_wide;              // keys of a chunk
+  int seq, tiles, chunks, slots;  // of this lane's sequence: number, tiles, chunks and partial results
+  SeqSpan q;
+  int upto, slots_to;             // items (or groups of rows) and partial results up to it in its block of 64
+
+  __device__ __forceinline__ bool is_wide(const SeqSpan& x) const { return KG > 0 && (long long)x.n * group > kFewRows; }
+  __device__ __forceinline__ int n_tiles(const SeqSpan& x) const {
+    const int rows = is_wide(x) ? wide_rows<KG>() : 32;
+    return (int)(((long long)x.n * group + rows - 1) / rows);
   }
-  const int c_few = max((it.c + 63) / 64 * 64, a.min_chunk), c_wide = max((it.c / wide_cost<KG>() + 128) / 128 * 128, 2 * a.min_chunk);
-  it.s = -1;
-  int before = 0, slots_before = 0;
-  for (int s0 = 0; s0 < b.n_seq; s0 += 64) {
-    if (s0 > 0) {
-      q = span(s0 + lane);
-      tiles = n_tiles(q);
-    }
+  __device__ __forceinline__ void read(int s0) {
+    seq = s0 + lane;
+    q = seq_span(a.b, min(seq, a.b.n_seq - 1));
+    if (seq >= a.b.n_seq) q.n = q.len = 0;
+    tiles = n_tiles(q);
+  }
+  __device__ __forceinline__ void count() {
     const int c = is_wide(q) ? c_wide : c_few, per = is_wide(q) ? wide_rows<KG>() / 32 : 1;
-    const int chunks = max((q.len + c - 1) / c, 1), items = tiles * chunks, slots = chunks > 1 ? items * per : 0;
-    const int count = JOIN ? (chunks > 1 ? tiles * per : 0) : items;
-    const int upto = scan64(count) + before, slots_to = a.max_chunks > 1 ? scan64(slots) + slots_before : 0;
-    const unsigned long long past = __ballot(upto > index);
-    if (past != 0) {
-      const int at = __ffsll(past) - 1;
-      auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
-      it.s = s0 + at;
-      it.tiles = of(tiles);
-      it.n_chunks = of(chunks);
-      it.first_slot = of(slots_to - slots);
-      it.q.first = of(q.first);
-      it.q.n = of(q.n);
-      it.q.len = of(q.len);
-      it.wide = is_wide(it.q);
-      it.c = it.wide ? c_wide : c_few;
-      it.slots = it.wide ? wide_rows<KG>() / 32 : 1;
-      const int local = index - of(upto - count);
-      if constexpr (JOIN) {
-        it.chunk = 0;
-        it.tile = local / it.slots;
-        *rows32 = local % it.slots;
-      } else {
-        it.chunk = local / it.tiles;
-        it.tile = it.tiles - 1 - local % it.tiles;
-      }
-      if (local < 0 || it.chunk >= it.n_chunks || it.tile >= it.tiles) it.s = -1;  // counts that have overflowed: see has_room
-      return it;
-    }
-    before = last_of(upto);
-    slots_before = last_of(slots_to);
+    chunks = a.max_chunks > 1 ? max((q.len + c - 1) / c, 1) : 1;
+    slots = chunks > 1 ? tiles * chunks * per : 0;
+    upto = scan64(JOIN ? (chunks > 1 ? tiles * per : 0) : tiles * chunks);
+    slots_to = a.max_chunks > 1 ? scan64(slots) : 0;
   }
-  return it;
-}
+
+  __device__ __forceinline__ Items(const PagedAttnLaunch& a_) : a(a_), lane(threadIdx.x & 63), group(a_.hq / a_.hkv) {
+    read(0);
+    c_few = c_wide = 0;
+    if (a.max_chunks > 1) {
+      // keys of a chunk of 32 rows: the cost of all tiles and heads over the number of workgroups (2^target_log2); a wide tile's
+      // are fewer by what it costs more
+      unsigned long long total = 0;
+      for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
+        if (s0 > 0) read(s0);
+        total += (unsigned long long)tiles * q.len * (is_wide(q) ? wide_cost<KG>() : 1);
+      }
+      if (a.b.n_seq > 64) read(0);
+      // lane by lane in two halves: sums of 64 numbers below 2^24 and of their upper parts
+      const unsigned long long high = (unsigned)last_of(scan64((int)(total >> 24)));
+      total = ((high << 24) + (unsigned)last_of(scan64((int)(total & 0xFFFFFF)))) * a.hkv;
+      const int share = (int)min((total + (1ull << a.target_log2) - 1) >> a.target_log2, 0x40000000ull);
+      c_few = max((share + 63) / 64 * 64, a.min_chunk);
+      c_wide = max((share / wide_cost<KG>() + 128) / 128 * 128, 2 * a.min_chunk);
+    }
+    if (KG > 0 && a.b.n_seq > 1 && a.b.n_seq <= 64) {
+      int rank = 0;
+      for (int j = 0; j < a.b.n_seq; ++j) {
+        const int other = __builtin_amdgcn_readlane(q.len, j);
+        rank += other > q.len || (other == q.len && j < lane) ? 1 : 0;
+      }
+      auto move = [&](int x) { return __builtin_amdgcn_ds_permute(rank * 4, x); };
+      if (lane >= a.b.n_seq) rank = lane;
+      seq = move(seq);
+      q.first = move(q.first);
+      q.n = move(q.n);
+      q.len = move(q.len);
+      tiles = move(tiles);
+    }
+    count();
+  }
+
+  // Groups of rows in all (JOIN).
+  __device__ __forceinline__ int total() {
+    int n = last_of(upto);
+    for (int s0 = 64; s0 < a.b.n_seq; s0 += 64) {
+      read(s0);
+      count();
+      n += last_of(upto);
+    }
+    return n;
+  }
+
+  __device__ __forceinline__ Item find(int index, int* rows32 = nullptr) {
+    Item it;
+    it.s = -1;
+    int before = 0, slots_before = 0;
+    for (int s0 = 0; s0 < a.b.n_seq; s0 += 64) {
+      if (a.b.n_seq > 64) {
+        read(s0);
+        count();
+      }
+      const unsigned long long past = __ballot(upto + before > index);
+      if (past != 0) {
+        const int at = __ffsll(past) - 1;
+        auto of = [&](int x) { return __builtin_amdgcn_readlane(x, at); };
+        it.s = of(seq);
+        it.tiles = of(tiles);
+        it.n_chunks = of(chunks);
+        it.q.first = of(q.first);
+        it.q.n = of(q.n);
+        it.q.len = of(q.len);
+        it.wide = is_wide(it.q);
+        it.c = a.max_chunks > 1 ? ((it.q.len + it.n_chunks - 1) / it.n_chunks + 127) / 128 * 128 : 0x40000000;  // even ones
+        it.slots = it.wide ? wide_rows<KG>() / 32 : 1;
+        it.first_slot = slots_before + of(slots_to - slots);
+        const int mine = JOIN ? it.tiles * it.slots : it.tiles * it.n_chunks, local = index - (before + of(upto) - mine);
+        if constexpr (JOIN) {
+          it.chunk = 0;
+          it.tile = local / it.slots;
+          *rows32 = local % it.slots;
+        } else {
+          it.chunk = local / it.tiles;
+          it.tile = it.tiles - 1 - local % it.tiles;
+        }
+        // counts that have overflowed, and prefix sums that go backwards and so ask for more room than the batch's rows do
+        if (local < 0 || it.chunk >= it.n_chunks || it.tile >= it.tiles) it.s = -1;
+        if (it.n_chunks > 1 && (it.first_slot < 0 || (long long)it.first_slot + (long long)it.tiles * it.n_chunks * it.slots > a.max_slots))
+          it.s = -1;
+        return it;
+      }
+      before += last_of(upto);
+      slots_before += last_of(slots_to);
+    }
+    return it;
+  }
+};
 
 // First slot of a (tile, chunk)'s partial result (one of every KV head stands there), and the row of part_lse and part_o that
 // one head's begins at.
@@ -129,11 +175,6 @@ __device__ __forceinline__ int part_slot(const Item& it, int chunk) {
 __device__ __forceinline__ long long part_row(const PagedAttnLaunch& a, const Item& it, int chunk, int kvh) {
   return ((long long)part_slot(it, chunk) * a.hkv + (long long)kvh * it.slots) * a.tile_rows;
 }
-// Prefix sums that go backwards can ask for more room than the batch's rows do; what has none is left out.
-__device__ __forceinline__ bool has_room(const PagedAttnLaunch& a, const Item& it) {
-  return it.n_chunks == 1 || (part_slot(it, 0) >= 0 && part_slot(it, it.n_chunks - 1) + it.slots <= a.max_slots);
-}
-
 // Where the keys and values of a sequence's KV head lie.
 template <bool PAGED>
 struct KvSource {
@@ -301,62 +342,88 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
   }
 }
 
-// out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse): one wave per row, two chunks at a time (one per half-wave at d = 128, and
-// four channels a lane).
+// out = sum_c w_c part_o[c], w_c = 2^(lse_c - lse).  D / 4 threads take a row's channels, four each; they are a row's only group
+// of threads where there are few chunks, and the workgroup's groups share a row's chunks where there are many: a group that walks
+// 512 chunks spends a trip to memory on every eight.  Chunks without mass (lse = -inf)
+// have outputs of zero.
 template <int D, bool BF16, int KG>
 __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
-  constexpr int LPR = D / 4, CG = 64 / LPR;  // lanes per row, chunks at a time
-  const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
-  const int kvh = blockIdx.x % a.hkv;
-  int rows32 = 0;
-  const Item it = find_item<KG, true>(a, group, blockIdx.x / a.hkv, lane, &rows32);
-  if (it.s < 0 || !has_room(a, it)) return;
-  const int tile0 = it.tile * 32 * it.slots, n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
-  for (int row = rows32 * 32 + uniform(blockIdx.y * 4 + (threadIdx.x >> 6)); row < n_rows; row += 4 * gridDim.y) {
-    const int rr = tile0 + row;
-    const int c4 = lane % LPR, cg = lane / LPR;
-    auto at = [&](int c) { return part_row(a, it, c, kvh) + row; };
+  constexpr int LPR = D / 4, NG = 256 / LPR, U = 8;  // threads and groups of threads per row, chunks requested at once
+  __shared__ f32x4 s_acc[256];
+  __shared__ float s_m[256], s_den[256];
+  const int group = a.hq / a.hkv, c4 = threadIdx.x % LPR, g = threadIdx.x / LPR;
+  // one row of a group and head after the other; few chunks: every eighth (sixteenth at d = 64) with those behind it
+  Items<KG, true> items(a);
+  const int heads = min(max(items.total(), 0), a.max_slots / 2) * a.hkv, rows = heads * a.tile_rows;
+  for (int u = blockIdx.x; u < rows; u += gridDim.x) {
+    int rows32 = 0;
+    const int r = u / heads, kvh = u % heads % a.hkv;
+    const Item it = items.find(u % heads / a.hkv, &rows32);
+    if (it.s < 0) continue;
+    const int tile0 = it.tile * 32 * it.slots, row0 = rows32 * 32 + r, n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
+    const bool many = it.n_chunks > U;
+    if (row0 >= n_rows || (!many && r % NG != 0)) continue;
+    const int from = many ? g : 0, by = many ? NG : 1;
+    const int row = min(many ? row0 : row0 + g, n_rows - 1);
+    const long long at0 = part_row(a, it, 0, kvh) + row, apart = (long long)it.tiles * it.slots * a.hkv * a.tile_rows;
     float m = -INFINITY, den = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c0 = 0; c0 < it.n_chunks; c0 += 64) {
-      const float l = c0 + lane < it.n_chunks ? a.part_lse[at(c0 + lane)] : -INFINITY;
-      float mx = l;
+    for (int c = from; c < it.n_chunks; c += by * U) {
+      float l[U];
+      f32x4 x[U];
 #pragma unroll
-      for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
-      const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = __builtin_amdgcn_exp2f(m - m_use), wt = __builtin_amdgcn_exp2f(l - m_use);
-      float sum = wt;
+      for (int u = 0; u < U; ++u) {
+        const long long at = at0 + min(c + u * by, it.n_chunks - 1) * apart;
+        l[u] = a.part_lse[at];
+        x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c4 * 4);
+      }
+      float top = m;
 #pragma unroll
-      for (int w = 1; w < 64; w *= 2) sum += __shfl_xor(sum, w);
-      den = fmaf(den, alpha, sum);
+      for (int u = 0; u < U; ++u) {
+        if (c + u * by >= it.n_chunks) l[u] = -INFINITY;
+        top = fmaxf(top, l[u]);
+      }
+      const float use = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - use);
+      m = top;
+      den *= alpha;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] *= alpha;
-      m = m_new;
-      const int n = min(64, it.n_chunks - c0);
-      constexpr int U = 4;  // requests ahead
-      for (int c = 0; c < n; c += U * CG) {
-        f32x4 x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at(c0 + min(c + u * CG + cg, n - 1)) * D + c4 * 4);
+      for (int u = 0; u < U; ++u) {
+        if (c + u * by >= it.n_chunks) continue;
+        const float w = __builtin_amdgcn_exp2f(l[u] - use);
+        den += w;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int mine = c + u * CG + cg;
-          const float f = __shfl(wt, min(mine, 63));
-          if (mine < n) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, x[u][e], acc[e]);
-          }
-        }
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[u][e], acc[e]);
       }
     }
+    if (many) {
+      s_acc[threadIdx.x] = acc;
+      s_m[threadIdx.x] = m;
+      s_den[threadIdx.x] = den;
+      __syncthreads();
+      float top = -INFINITY;
 #pragma unroll
-    for (int w = LPR; w < 64; w *= 2)
+      for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[c4 + i * LPR]);
+      const float use = top == -INFINITY ? 0.f : top;
+      m = top;
+      den = 0.f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], w);
-    if (cg > 0) continue;
+      for (int e = 0; e < 4; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int from_i = c4 + i * LPR;
+        const float w = __builtin_amdgcn_exp2f(s_m[from_i] - use);
+        den = fmaf(w, s_den[from_i], den);
+        const f32x4 x = s_acc[from_i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+      }
+      __syncthreads();
+    }
+    if (many ? g > 0 : row0 + g >= n_rows) continue;
     const float inv = den == 0.f ? 0.f : 1.f / den;
-    const int tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+    const int rr = tile0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
     char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
     if constexpr (BF16) {
       const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
@@ -373,8 +440,9 @@ __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
 
 template <int D, bool BF16>
 hipError_t launch_join(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
-  // a tile that is cut has two slots at least
-  const dim3 grid((unsigned)(p.max_slots / 2 * a.hkv), (unsigned)(p.kg > 0 ? 1 : (p.tile_rows + 3) / 4));
+  // a tile that is cut has two slots at least; no more workgroups than are resident at once
+  const long long rows = (long long)(p.max_slots / 2) * a.hkv * p.tile_rows;
+  const dim3 grid((unsigned)(rows < 1024 ? rows : 1024));
   if (p.kg == 2) hipLaunchKernelGGL((k_join_chunks<D, BF16, 2>), grid, dim3(256), 0, s, a);
   else if (p.kg == 1) hipLaunchKernelGGL((k_join_chunks<D, BF16, 1>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_join_chunks<D, BF16, 0>), grid, dim3(256), 0, s, a);

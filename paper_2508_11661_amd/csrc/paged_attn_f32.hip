@@ -138,8 +138,8 @@ __device__ __forceinline__ void attend_f32(const PagedAttnLaunch& a, const Item&
 template <int D, bool PAGED>
 __global__ __launch_bounds__(64 * NW, 2) void k_attend_f32(PagedAttnLaunch a) {
   const int index = blockIdx.x / a.hkv, kvh = blockIdx.x % a.hkv;
-  const Item it = find_item<0, false>(a, a.hq / a.hkv, index, threadIdx.x & 63);
-  if (it.s < 0 || !has_room(a, it)) return;
+  const Item it = Items<0, false>(a).find(index);
+  if (it.s < 0) return;
   attend_f32<D, PAGED>(a, it, kvh);
 }
 
