@@ -685,7 +685,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   auto less = [](long long x, long long y) { return x < y ? x : y; };
   p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv) : prompt_shape(rows * hkv, n_rows / n, max_len);
   p.once = most <= 32;
-  p.target_log2 = 9;  // workgroups: as many as are resident at once, of wide tiles twice as many, for evenness
+  p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
   p.min_chunk = 256;
   const long long wide = p.kg == 2 ? 128 : 256;
   p.joins = paged && max_len > p.min_chunk;  // prompts have rows enough: the join would be one more launch

@@ -352,89 +352,91 @@ __global__ __launch_bounds__(256) void k_join_chunks(PagedAttnLaunch a) {
   __shared__ f32x4 s_acc[256];
   __shared__ float s_m[256], s_den[256];
   const int group = a.hq / a.hkv, c4 = threadIdx.x % LPR, g = threadIdx.x / LPR;
-  // one row of a group and head after the other; few chunks: every eighth (sixteenth at d = 64) with those behind it
+  // A workgroup takes a part of the rows of a group and head: of one where there are enough of them.
   Items<KG, true> items(a);
-  const int heads = min(max(items.total(), 0), a.max_slots / 2) * a.hkv, rows = heads * a.tile_rows;
-  for (int u = blockIdx.x; u < rows; u += gridDim.x) {
+  const int heads = min(max(items.total(), 0), a.max_slots / 2) * a.hkv;
+  const int parts = heads >= (int)gridDim.x ? 1 : min((int)gridDim.x / max(heads, 1), a.tile_rows);
+  for (int u = blockIdx.x; u < heads * parts; u += gridDim.x) {
     int rows32 = 0;
-    const int r = u / heads, kvh = u % heads % a.hkv;
-    const Item it = items.find(u % heads / a.hkv, &rows32);
+    const int head = u % heads, kvh = head % a.hkv;
+    const Item it = items.find(head / a.hkv, &rows32);
     if (it.s < 0) continue;
-    const int tile0 = it.tile * 32 * it.slots, row0 = rows32 * 32 + r, n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
+    const int tile0 = it.tile * 32 * it.slots, n_rows = min(it.q.n * group - tile0, 32 * (rows32 + 1));
     const bool many = it.n_chunks > U;
-    if (row0 >= n_rows || (!many && r % NG != 0)) continue;
-    const int from = many ? g : 0, by = many ? NG : 1;
-    const int row = min(many ? row0 : row0 + g, n_rows - 1);
-    const long long at0 = part_row(a, it, 0, kvh) + row, apart = (long long)it.tiles * it.slots * a.hkv * a.tile_rows;
-    float m = -INFINITY, den = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int c = from; c < it.n_chunks; c += by * U) {
-      float l[U];
-      f32x4 x[U];
+    const int from = many ? g : 0, by = many ? NG : 1, step = many ? 1 : NG;
+    for (int row0 = rows32 * 32 + u / heads * step; row0 < n_rows; row0 += parts * step) {
+      const int row = min(many ? row0 : row0 + g, n_rows - 1);
+      const long long at0 = part_row(a, it, 0, kvh) + row, apart = (long long)it.tiles * it.slots * a.hkv * a.tile_rows;
+      float m = -INFINITY, den = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      for (int c = from; c < it.n_chunks; c += by * U) {
+        float l[U];
+        f32x4 x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const long long at = at0 + min(c + u * by, it.n_chunks - 1) * apart;
-        l[u] = a.part_lse[at];
-        x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c4 * 4);
+        for (int u = 0; u < U; ++u) {
+          const long long at = at0 + min(c + u * by, it.n_chunks - 1) * apart;
+          l[u] = a.part_lse[at];
+          x[u] = *reinterpret_cast<const f32x4*>(a.part_o + at * D + c4 * 4);
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (c + u * by >= it.n_chunks) l[u] = -INFINITY;
+          top = fmaxf(top, l[u]);
+        }
+        const float use = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - use);
+        m = top;
+        den *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= alpha;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (c + u * by >= it.n_chunks) continue;
+          const float w = __builtin_amdgcn_exp2f(l[u] - use);
+          den += w;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[u][e], acc[e]);
+        }
       }
-      float top = m;
+      if (many) {
+        s_acc[threadIdx.x] = acc;
+        s_m[threadIdx.x] = m;
+        s_den[threadIdx.x] = den;
+        __syncthreads();
+        float top = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (c + u * by >= it.n_chunks) l[u] = -INFINITY;
-        top = fmaxf(top, l[u]);
+        for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[c4 + i * LPR]);
+        const float use = top == -INFINITY ? 0.f : top;
+        m = top;
+        den = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int from_i = c4 + i * LPR;
+          const float w = __builtin_amdgcn_exp2f(s_m[from_i] - use);
+          den = fmaf(w, s_den[from_i], den);
+          const f32x4 x = s_acc[from_i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        }
+        __syncthreads();
       }
-      const float use = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - use);
-      m = top;
-      den *= alpha;
+      if (many ? g > 0 : row0 + g >= n_rows) continue;
+      const float inv = den == 0.f ? 0.f : 1.f / den;
+      const int rr = tile0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
+      char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
+      if constexpr (BF16) {
+        const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
+        *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
+      } else {
+        f32x4 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] *= alpha;
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (c + u * by >= it.n_chunks) continue;
-        const float w = __builtin_amdgcn_exp2f(l[u] - use);
-        den += w;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[u][e], acc[e]);
+        for (int e = 0; e < 4; ++e) y[e] = acc[e] * inv;
+        *reinterpret_cast<f32x4*>(out + c4 * 16) = y;
       }
+      if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
     }
-    if (many) {
-      s_acc[threadIdx.x] = acc;
-      s_m[threadIdx.x] = m;
-      s_den[threadIdx.x] = den;
-      __syncthreads();
-      float top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) top = fmaxf(top, s_m[c4 + i * LPR]);
-      const float use = top == -INFINITY ? 0.f : top;
-      m = top;
-      den = 0.f;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = 0.f;
-#pragma unroll
-      for (int i = 0; i < NG; ++i) {
-        const int from_i = c4 + i * LPR;
-        const float w = __builtin_amdgcn_exp2f(s_m[from_i] - use);
-        den = fmaf(w, s_den[from_i], den);
-        const f32x4 x = s_acc[from_i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
-      }
-      __syncthreads();
-    }
-    if (many ? g > 0 : row0 + g >= n_rows) continue;
-    const float inv = den == 0.f ? 0.f : 1.f / den;
-    const int rr = tile0 + row, tok = it.q.first + rr / group, hd = kvh * group + rr % group;
-    char* out = a.out.p + hd * a.out.hs + tok * a.out.rs;
-    if constexpr (BF16) {
-      const bf16x4 y = {(__bf16)(acc[0] * inv), (__bf16)(acc[1] * inv), (__bf16)(acc[2] * inv), (__bf16)(acc[3] * inv)};
-      *reinterpret_cast<bf16x4*>(out + c4 * 8) = y;
-    } else {
-      f32x4 y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = acc[e] * inv;
-      *reinterpret_cast<f32x4*>(out + c4 * 16) = y;
-    }
-    if (c4 == 0 && a.lse != nullptr) a.lse[(long long)hd * a.b.n_rows + tok] = (m + __log2f(den)) * kLn2;
   }
 }
 
@@ -442,7 +444,7 @@ template <int D, bool BF16>
 hipError_t launch_join(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStream_t s) {
   // a tile that is cut has two slots at least; no more workgroups than are resident at once
   const long long rows = (long long)(p.max_slots / 2) * a.hkv * p.tile_rows;
-  const dim3 grid((unsigned)(rows < 1024 ? rows : 1024));
+  const dim3 grid((unsigned)(rows < 1536 ? rows : 1536));
   if (p.kg == 2) hipLaunchKernelGGL((k_join_chunks<D, BF16, 2>), grid, dim3(256), 0, s, a);
   else if (p.kg == 1) hipLaunchKernelGGL((k_join_chunks<D, BF16, 1>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_join_chunks<D, BF16, 0>), grid, dim3(256), 0, s, a);
