@@ -72,7 +72,8 @@ struct PagedAttnLaunch {
   RowsArg k, v;  // pages: hs = bytes of one head's rows of a page, rs = bytes of a row
   float* lse;    // may be null
   float scale;
-  int target_log2, min_chunk;  // workgroups to share the keys out over; no chunk is shorter than min_chunk keys (wide tiles: twice that)
+  int target_log2, ragged_log2;  // workgroups to share the keys out over, and where sequences differ in length
+  int min_chunk;          // no chunk is shorter than min_chunk keys (wide tiles: twice that)
   int max_chunks;         // 1: no sequence's keys are cut
   // partial results of the tiles whose keys are cut, in slots of 32 rows (of tile_rows, where no tile has more)
   int max_slots, tile_rows;
@@ -85,7 +86,7 @@ hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
 struct PagedAttnPlan {
   int kg;     // which wide tiles there are: see paged_attn.hpp
   bool once;  // every sequence is one tile of 32 rows
-  int target_log2, min_chunk, max_items, max_slots, tile_rows;
+  int target_log2, ragged_log2, min_chunk, max_items, max_slots, tile_rows;
   bool joins;  // whether any sequence can have more than one chunk
   size_t part_lse, bytes;  // workspace: part_o, then part_lse
 };

@@ -689,10 +689,11 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   p.min_chunk = 256;
   const long long wide = p.kg == 2 ? 128 : 256;
   p.joins = paged && max_len > p.min_chunk;  // prompts have rows enough: the join would be one more launch
-  // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-target_log2 of the keys that
+  // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-ragged_log2 of the keys that
   // the tiles of all heads see).
-  const long long tile = p.kg > 0 ? wide : 32, shares = ((1 << p.target_log2) + hkv - 1) / hkv;
-  const long long tiles = less(n * ((most + tile - 1) / tile), rows / tile + n);
+  const long long tile = p.kg > 0 ? wide : 32, tiles = less(n * ((most + tile - 1) / tile), rows / tile + n);
+  p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? 10 : p.target_log2;  // fewer have many chunks each
+  const long long shares = ((1 << p.ragged_log2) + hkv - 1) / hkv;
   p.max_items = (int)(tiles + (p.joins ? shares : 0));
   // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
   p.max_slots = (int)(p.joins ? less(p.max_items, 2 * shares) * (tile / 32) : 0);

@@ -1033,7 +1033,7 @@ static int place_parts(PagedAttnLaunch* a, void* ws, size_t ws_bytes) {
   const PagedAttnPlan p = paged_attn_plan(a->dtype, a->d, a->hq, a->hkv, a->b.n_seq, a->b.n_rows, a->b.max_new, a->b.max_len,
                                           a->paged != 0);
   if (!enough(ws, ws_bytes, p.bytes)) return SAMKV_EWORKSPACE;
-  a->target_log2 = p.target_log2; a->min_chunk = p.min_chunk; a->max_slots = p.max_slots; a->tile_rows = p.tile_rows;
+  a->target_log2 = p.target_log2; a->ragged_log2 = p.ragged_log2; a->min_chunk = p.min_chunk; a->max_slots = p.max_slots; a->tile_rows = p.tile_rows;
   a->max_chunks = p.joins ? 0x7FFFFFFF : 1;
   a->part_o = static_cast<float*>(ws);
   a->part_lse = reinterpret_cast<float*>(static_cast<char*>(ws) + p.part_lse);

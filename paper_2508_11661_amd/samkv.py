@@ -518,23 +518,23 @@ def _current_device() -> int:
     return torch.cuda.current_device() if _device is None else _device()
 
 
-def _rows(t: torch.Tensor, heads: int, n: int, d: int, dtype: torch.dtype, device: int) -> _Rows:
-    assert tuple(t.shape) == (heads, n, d), f"{tuple(t.shape)} instead of {(heads, n, d)}"
-    assert t.dtype == dtype and t.is_cuda and t.get_device() == device, "dtype or device of a row tensor"
-    s = t.stride()
-    assert s[2] == 1, "the last dimension must be dense"
-    return _Rows(t.data_ptr(), s[0] if heads > 1 else 0, s[1] if n > 1 else 0)
+def _rows(t: torch.Tensor, shape: Tuple[int, int, int], dtype: torch.dtype, device: int) -> _Rows:
+    assert t.shape == shape, f"{tuple(t.shape)} instead of {shape}"
+    assert t.dtype is dtype and t.get_device() == device, "dtype or device of a row tensor"
+    head, row, last = t.stride()
+    assert last == 1, "the last dimension must be dense"
+    return _Rows(t.data_ptr(), head if shape[0] > 1 else 0, row if shape[1] > 1 else 0)
 
 
 def _int32(t: torch.Tensor, n: int, device: int) -> int:
-    assert t.dtype == torch.int32 and t.is_cuda and t.get_device() == device and t.is_contiguous() and t.numel() == n
+    assert t.dtype is torch.int32 and t.get_device() == device and t.is_contiguous() and t.numel() == n
     return t.data_ptr()
 
 
 def _lse(t: Optional[torch.Tensor], heads: int, n: int, device: int) -> Optional[int]:
     if t is None:
         return None
-    assert t.dtype == torch.float32 and tuple(t.shape) == (heads, n) and t.is_contiguous() and t.get_device() == device
+    assert t.dtype is torch.float32 and t.shape == (heads, n) and t.is_contiguous() and t.get_device() == device
     return t.data_ptr()
 
 
@@ -542,7 +542,7 @@ def _scratch(ws: Optional[torch.Tensor], device: int) -> Tuple[Optional[int], in
     if ws is None:
         return None, 0
     assert ws.is_contiguous() and ws.get_device() == device
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 class PagedCache:
@@ -551,7 +551,7 @@ class PagedCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         assert k.is_cuda and k.dim() == 4 and k.is_contiguous() and v.is_contiguous()
         assert v.shape == k.shape and v.dtype == k.dtype and v.device == k.device
-        self.k, self.v, self.device = k, v, k.get_device()
+        self.k, self.v, self.device, self.dtype = k, v, k.get_device(), k.dtype
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = k.shape
         self.c = _Pages(self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, _dtype_code(k.dtype), k.data_ptr(),
                         v.data_ptr())
@@ -564,7 +564,7 @@ class PagedBatch:
 
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, max_len: int, cu_new: Optional[torch.Tensor] = None,
                  max_new: int = 1, n_new: Optional[int] = None):
-        assert table.is_cuda and table.dim() == 2
+        assert table.is_cuda and lens.is_cuda and table.dim() == 2
         n_seq, max_pages = table.shape
         self.device = table.get_device()
         self.n_new = n_seq * max_new if n_new is None else n_new
@@ -596,10 +596,12 @@ def samkv_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu: to
     hq, n, d = q.shape
     hkv, dt = k.shape[0], q.dtype
     n_seq = cu.numel() - 1
+    assert d > 0 and q.is_cuda
     p, n_bytes = _scratch(ws, dev)
-    _check(_lib.samkv_prefill_attn(_rows(q, hq, n, d, dt, dev), _rows(k, hkv, n, d, dt, dev), _rows(v, hkv, n, d, dt, dev),
+    rows, kv = (hq, n, d), (hkv, n, d)
+    _check(_lib.samkv_prefill_attn(_rows(q, rows, dt, dev), _rows(k, kv, dt, dev), _rows(v, kv, dt, dev),
                                    _int32(cu, n_seq + 1, dev), n_seq, n, max_len, hq, hkv, d, _dtype_code(dt), scale,
-                                   _rows(out, hq, n, d, dt, dev), _lse(lse, hq, n, dev), p, n_bytes, _stream()),
+                                   _rows(out, rows, dt, dev), _lse(lse, hq, n, dev), p, n_bytes, _stream()),
            "samkv_prefill_attn")
 
 
@@ -609,14 +611,14 @@ def samkv_paged_append(cache: PagedCache, batch: PagedBatch, k_new: torch.Tensor
     """Pages <- k_new (rotated), v_new [Hkv, n_new, d]; q_out [Hq, n_new, d] <- q rotated (q_out may be q)."""
     dev = _current_device()
     assert cache.device == batch.device == dev
-    n, d, dt = batch.n_new, cache.head_dim, cache.k.dtype
+    n, d, dt = batch.n_new, cache.head_dim, cache.dtype
     if rope is not None:
         assert rope.device == dev and (rope.positions is None or rope.positions.numel() == n)
+    kv = (cache.n_kv_heads, n, d)
     hq = 0 if q is None else q.shape[0]
-    _check(_lib.samkv_paged_append(cache.c, batch.c, _rows(k_new, cache.n_kv_heads, n, d, dt, dev),
-                                   _rows(v_new, cache.n_kv_heads, n, d, dt, dev), None if rope is None else rope.c,
-                                   None if q is None else _rows(q, hq, n, d, dt, dev),
-                                   None if q_out is None else _rows(q_out, hq, n, d, dt, dev), hq, _stream()),
+    _check(_lib.samkv_paged_append(cache.c, batch.c, _rows(k_new, kv, dt, dev), _rows(v_new, kv, dt, dev),
+                                   None if rope is None else rope.c, None if q is None else _rows(q, (hq, n, d), dt, dev),
+                                   None if q_out is None else _rows(q_out, (hq, n, d), dt, dev), hq, _stream()),
            "samkv_paged_append")
 
 
@@ -629,10 +631,10 @@ def samkv_paged_attn(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scal
     """out [Hq, n_new, d] in the cache's dtype, lse [Hq, n_new] float32 <- attention of the new tokens over the pages."""
     dev = _current_device()
     assert cache.device == batch.device == dev
-    hq, n, d = q.shape[0], batch.n_new, cache.head_dim
-    dt = cache.k.dtype
+    hq, n, dt = q.shape[0], batch.n_new, cache.dtype
+    rows = (hq, n, cache.head_dim)
     p, n_bytes = _scratch(ws, dev)
-    _check(_lib.samkv_paged_attn(cache.c, batch.c, _rows(q, hq, n, d, dt, dev), hq, scale, _rows(out, hq, n, d, dt, dev),
+    _check(_lib.samkv_paged_attn(cache.c, batch.c, _rows(q, rows, dt, dev), hq, scale, _rows(out, rows, dt, dev),
                                  _lse(lse, hq, n, dev), p, n_bytes, _stream()), "samkv_paged_attn")
 
 
