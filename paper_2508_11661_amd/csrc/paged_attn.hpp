@@ -45,8 +45,9 @@ struct Item {
 
 // Finds work items: JOIN = false, number `index` of them; JOIN = true, group of 32 rows number `index` among the tiles whose keys
 // are cut (the chunk is the first).  All calls are by whole waves, and the results are the same in every lane.  A lane holds one
-// of 64 sequences; batches of up to that many are read once, and their wide tiles taken in order of falling length, so that a long
-// sequence's are not the last to start.  Within a sequence items run chunk by chunk, the last tile (with the most keys) first.
+// of 64 sequences; batches of up to that many are read once, and over a cache wide tiles are taken in order of falling length, so
+// that a long sequence's are not the last to start (24 sequences, three of them with 1024 new tokens: 447 -> 437 us; prompts gain
+// less than the order costs, 2 %).  Within a sequence items run chunk by chunk, the last tile (with the most keys) first.
 template <int KG, bool JOIN>
 struct Items {
   const PagedAttnLaunch& a;
@@ -101,7 +102,7 @@ struct Items {
       c_few = max((share + 63) / 64 * 64, a.min_chunk);
       c_wide = max((share / wide_cost<KG>() + 128) / 128 * 128, 2 * a.min_chunk);
     }
-    if (KG > 0 && a.b.n_seq > 1 && a.b.n_seq <= 64) {
+    if (KG > 0 && a.paged && a.b.n_seq > 1 && a.b.n_seq <= 64) {
       int rank = 0;
       for (int j = 0; j < a.b.n_seq; ++j) {
         const int other = __builtin_amdgcn_readlane(q.len, j);
