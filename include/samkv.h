@@ -367,7 +367,11 @@ int samkv_kv_update(void* k_c, void* v_c, const void* k_new, const void* v_new, 
  *     The host passes bounds for them (max_len, max_new).  Whatever the arrays hold, no access leaves the tensors: a
  *     length beyond its bound counts as the bound, a negative one as zero, a sequence's rows end at the tensors' last row, and
  *     page numbers outside [0, n_pages) are taken as the nearest page when they are read and not written to at all.
- *     Sequences are packed one behind the other; rows behind the last one are neither read nor written. */
+ *     Sequences are packed one behind the other; rows behind the last one are not written (and what they hold reaches
+ *     nothing);
+ *   - counts and bounds are at least 1 (SAMKV_EINVAL).  n_q_heads * rows is at most 2^23 - 1, a grid at most 2^32 - 1 threads
+ *     (SAMKV_EUNSUPPORTED).
+ * A device's first attention call (of these or of those above) sets up its kernels and must not be captured into a graph. */
 #define SAMKV_MAX_SEQ 4096
 typedef struct {
   void* p;
@@ -411,9 +415,14 @@ typedef struct {
  *   be NULL.  cu  device [n_seq + 1]: sequence s is rows cu[s] .. cu[s + 1] - 1.  max_len: bound of the sequences' lengths, rows
  *   of a longer one past the bound are left as they were.
  * This is the prefill that gives the per-document caches of samkv_caches.  Keys and values of later rows do not reach a row
- * whatever they hold (infinities and NaN included).
- * Arithmetic: float32 scores, statistics and sums.
- * ws: samkv_prefill_workspace_bytes(...) bytes, 256-byte aligned. */
+ * whatever they hold (infinities and NaN included; rows beside infinities or NaN among values are computed a second time one by
+ * one, which can make a call some hundred times slower).  out must not overlap q, k or v (the same address: SAMKV_EINVAL).
+ * row_stride of k and v is below 2^24 bytes (SAMKV_EUNSUPPORTED).
+ * Arithmetic: scores, maxima, sums and outputs are float32.  float32: products are float32.  bf16: products of bf16 values are
+ * exact; a softmax weight enters its product with v rounded to 16 significant bits (two bf16 terms) where sequences are taken in
+ * tiles of 32 rows, and to bf16 (2^-8 of its value at most, its sum over the keys being that of the unrounded weights) in wide
+ * tiles; which those are follows from the bounds, not from the data.  Equal calls give equal bits.
+ * ws: samkv_prefill_workspace_bytes(...) bytes, 256-byte aligned; 0 bytes are needed today, and NULL is taken then. */
 size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t dtype);
 int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_rows* v, const int32_t* cu, int32_t n_seq,
@@ -426,8 +435,8 @@ int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_row
  *   q, q_out      n_q_heads of n_new rows, in the pages' dtype, q_out = q rotated; both NULL: no queries.  q_out may be q
  *                 itself (same address and strides); otherwise what is written must not overlap what is read.
  * Angles are reduced in float64, the rotation is float32 and rounded once.  A token without a slot, or whose page number is
- * outside [0, n_pages), is not written (its query still is rotated, by its given position, or else by 0).  Two sequences that
- * write to one row of a shared page leave either's. */
+ * outside [0, n_pages), is not written (its query still is rotated, by its given position, or else by 0).  Tokens that are
+ * written to the same row of a page (of a page that two sequences share, say) leave a mixture of theirs there. */
 int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* k_new, const samkv_rows* v_new,
                        const samkv_rope* rope, const samkv_rows* q, const samkv_rows* q_out, int32_t n_q_heads, void* stream);
 
@@ -437,7 +446,8 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
  *   q, out  n_q_heads of n_new rows in the pages' dtype; lse float32 [n_q_heads][n_new], may be NULL.
  * One new token per sequence is a decoding step; several are drafted tokens or a chunk of a prompt; both mix in one batch.
  * A token without a slot attends to nothing: out 0, lse -inf.  Slots behind a token do not reach it whatever they hold.
- * Arithmetic as in samkv_prefill_attn.
+ * Arithmetic as in samkv_prefill_attn; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long sequences are
+ * cut into chunks whose results are joined in float32; which chunks there are follows from the lengths alone.
  * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned. */
 size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads);
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,

@@ -52,7 +52,8 @@ union Frag {
   bf16x8 b;
   u32x4 u;
 };
-// ONCE: sequences are one tile, so that each K and V row is read once (64 x 4096 keys, 8 heads: 190 -> 169 us, 6.4 TB/s).
+// ONCE: sequences are one tile, so that each K and V row is read once (64 x 4096 keys, 8 heads: 192 -> 170 us, 6.3 TB/s; where
+// the sequences share all pages, 78 -> 79 us, 16 x 16384 keys 81 -> 88 us).
 template <int D, bool PAGED, int NW, bool ONCE>
 __device__ __forceinline__ void attend_few(const PagedAttnLaunch& a, const Item& it, int kvh) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -574,10 +575,10 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int j = 0; j < 16; ++j) sum += fabsf(o[i][j]);
-  const unsigned long long odd2 = __ballot(!(sum < INFINITY));
-  uint32_t odd = (uint32_t)odd2 | (uint32_t)(odd2 >> 32);  // rows whose outputs are not all finite
-  odd &= n_valid < 32 ? (1u << n_valid) - 1 : ~0u;
   const float l_tot = sum_across_halves(l_run), inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+  const unsigned long long odd2 = __ballot(l_tot == l_tot && !(sum < INFINITY));
+  uint32_t odd = (uint32_t)odd2 | (uint32_t)(odd2 >> 32);  // rows to be computed again
+  odd &= n_valid < 32 ? (1u << n_valid) - 1 : ~0u;
   const float lse2 = m_ref + __log2f(l_tot);
   auto again = [&]() {  // behind the wave's own stores
     for (; odd != 0; odd &= odd - 1) {
@@ -675,9 +676,10 @@ static int prompt_shape(long long rows, long long mean_len, int max_len) {
   return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
 }
 // New tokens over a cache, whose keys are cut into chunks until the chip is full: tiles of 32 rows where no sequence has more than
-// three of them (a wide tile costs about that), 128 where there are few rows (4 x 256 tokens over 3000, 32 heads: 115 / 62 / 78;
-// 2 x 512 over 8000: 264 / 138 / 153; 1 x 2048 over 16000: 953 / 508 / 486).
-static int paged_shape(long long most, long long rows) { return most <= 96 ? 0 : rows <= 49152 ? 2 : 1; }
+// two of them (8 sequences of 4000 keys, 32 heads over 8, 32-row / wide tiles, us: two 37.8 / 40.6, three 60 / 42; 32 of 2000, 8
+// heads over 2 of 64 channels: 24.5 / 28.2, 32.5 / 30.0), 128 rows where there are few of them (4 x 256 tokens over 3000, 32 heads,
+// 32 / 128 / 256 rows: 115 / 62 / 78; 2 x 512 over 8000: 264 / 138 / 153; 1 x 2048 over 16000: 953 / 508 / 486).
+static int paged_shape(long long most, long long rows) { return most <= 64 ? 0 : rows <= 49152 ? 2 : 1; }
 
 PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
@@ -691,7 +693,8 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   p.joins = paged && max_len > p.min_chunk;  // prompts have rows enough: the join would be one more launch
   // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-ragged_log2 of the keys that
   // the tiles of all heads see).
-  const long long tile = p.kg > 0 ? wide : 32, tiles = less(n * ((most + tile - 1) / tile), rows / tile + n);
+  const long long tile = p.kg > 0 ? wide : 32, with_rows = less(n, n_rows);  // sequences with rows
+  const long long tiles = less(with_rows * ((most + tile - 1) / tile), rows / tile + with_rows);
   p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? 10 : p.target_log2;  // fewer have many chunks each
   const long long shares = ((1 << p.ragged_log2) + hkv - 1) / hkv;
   p.max_items = (int)(tiles + (p.joins ? shares : 0));

@@ -201,13 +201,14 @@ struct KvSource {
   }
 };
 
-// One row of a sequence against the keys of its item's chunk by a wave, key by key, so that a value meets the weight of a row that
-// sees it and nothing else.  The matrix products multiply the values of keys that a row does not see by zero, and two-term weights
-// have terms of zero and of either sign: infinities and NaN among the values make NaN of the outputs of any row.  Rows whose outputs
-// are not all finite are therefore computed once more like this.
+// One row of a sequence against the keys of its item's chunk by a wave, so that a value meets the weight of a row that sees it and
+// nothing else.  The matrix products multiply the values of keys that a row does not see by zero, and two-term weights have terms
+// of zero and of either sign: infinities and NaN among the values make NaN of the outputs of any row.  Rows whose outputs are not
+// all finite are therefore computed once more like this, unless their sum is NaN: a score that they see is, and so is every output.
+// A lane takes a key for the scores, channels for the outputs.
 template <bool BF16, int D, bool PAGED>
 __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item& it, const KvSource<PAGED>& src, int r, int begin, int row) {
-  constexpr int CPL = D / 64;
+  constexpr int CPL = D / 64, PIECES = D * (BF16 ? 2 : 4) / 16, U = 8;
   const int lane = threadIdx.x & 63, group = a.hq / a.hkv;
   const int t = r / group, head = src.kvh * group + r % group, tok = it.q.first + t;
   const int end = min(min(it.q.len - it.q.n + t + 1, it.q.len), begin + it.c);
@@ -215,18 +216,25 @@ __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item&
     if constexpr (BF16) return __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(p)[c] << 16);
     else return reinterpret_cast<const float*>(p)[c];
   };
-  auto page_of = [&](int key) { return PAGED ? min(max(a.b.table[(long long)it.s * a.b.max_pages + (key >> a.b.page_log2)], 0), a.b.n_pages - 1) : 0; };
   const char* qr = a.q.p + head * a.q.hs + tok * a.q.rs;
   float m = -INFINITY, l = 0.f, o[CPL] = {};
+#pragma unroll 1
   for (int k0 = begin; k0 < end; k0 += 64) {
-    float x = -INFINITY;
-    if (k0 + lane < end) {
-      const char* kr = a.k.p + src.at(a.k, k0 + lane, page_of(k0 + lane));
-      float dot = 0.f;
+    const int n = min(64, end - k0), key = k0 + min(lane, n - 1);
+    int page = 0;
+    if constexpr (PAGED) page = min(max(a.b.table[(long long)it.s * a.b.max_pages + (key >> a.b.page_log2)], 0), a.b.n_pages - 1);
+    const char* kr = a.k.p + src.at(a.k, key, page);
+    float dot = 0.f;
 #pragma unroll 4
-      for (int c = 0; c < D; ++c) dot = fmaf(element(qr, c), element(kr, c), dot);
-      x = dot * a.scale;
+    for (int c = 0; c < PIECES; ++c) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(qr + c * 16), y = *reinterpret_cast<const u32x4*>(kr + c * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (BF16) dot = fmaf(bf16_hi(x[e]), bf16_hi(y[e]), fmaf(bf16_lo(x[e]), bf16_lo(y[e]), dot));
+        else dot = fmaf(__uint_as_float(x[e]), __uint_as_float(y[e]), dot);
+      }
     }
+    const float x = lane < n ? dot * a.scale : -INFINITY;
     float mx = x;
     for (int w = 1; w < 64; w *= 2) mx = fmaxf(mx, __shfl_xor(mx, w));
     const float m_new = fmaxf(m, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
@@ -237,10 +245,22 @@ __device__ __forceinline__ void attend_row(const PagedAttnLaunch& a, const Item&
     m = m_new;
     for (int e = 0; e < CPL; ++e) o[e] *= alpha;
 #pragma unroll 1
-    for (int j = 0; j < min(64, end - k0); ++j) {
-      const float w = __shfl(p, j);
-      const char* vr = a.v.p + src.at(a.v, k0 + j, page_of(k0 + j));
-      for (int e = 0; e < CPL; ++e) o[e] = fmaf(w, element(vr, lane + 64 * e), o[e]);
+    for (int j = 0; j < n; j += U) {
+      float y[U][CPL];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int at = min(j + u, n - 1);
+        const char* vr = a.v.p + src.at(a.v, k0 + at, __builtin_amdgcn_readlane(page, at));
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) y[u][e] = element(vr, lane + 64 * e);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (j + u < n) {
+          const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), min(j + u, 63)));
+#pragma unroll
+          for (int e = 0; e < CPL; ++e) o[e] = fmaf(w, y[u][e], o[e]);
+        }
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -318,7 +338,9 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] += y[e];
     }
-    const unsigned long long odd = __ballot(!(fabsf(x[0]) + fabsf(x[1]) + fabsf(x[2]) + fabsf(x[3]) < INFINITY));
+    float m;
+    const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
+    const unsigned long long odd = __ballot(l == l && !(fabsf(x[0]) + fabsf(x[1]) + fabsf(x[2]) + fabsf(x[3]) < INFINITY));
     if (odd != 0) {
 #pragma unroll 1
       for (int i = 0; i < RPW && row0 + i < n_valid; ++i)
@@ -327,8 +349,6 @@ __device__ __forceinline__ void join_waves(const PagedAttnLaunch& a, const Item&
       if (row0 + lane / LPR >= n_valid || (odd >> (lane / LPR * LPR) & ((1ull << LPR) - 1)) != 0) continue;
     }
     if (row0 + lane / LPR >= n_valid) continue;
-    float m;
-    const float l = joined(row, &m), inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] *= inv;
     const float lse2 = m + __log2f(l);

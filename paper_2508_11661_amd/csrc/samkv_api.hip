@@ -1028,10 +1028,13 @@ static int check_prompts(int n_seq, int n_tok, int max_len, int hq, int hkv, int
   return n_seq > SAMKV_MAX_SEQ || (long long)hq * n_tok > 0x7FFFFFFF / 256 ? SAMKV_EUNSUPPORTED : SAMKV_OK;
 }
 
+static bool fits(const PagedAttnPlan& p, int hkv) { return (long long)p.max_items * hkv * 512 <= 0xFFFFFFFFll; }  // threads of a grid
+
 // Plan and workspace of an attention launch whose sizes are set.
 static int place_parts(PagedAttnLaunch* a, void* ws, size_t ws_bytes) {
   const PagedAttnPlan p = paged_attn_plan(a->dtype, a->d, a->hq, a->hkv, a->b.n_seq, a->b.n_rows, a->b.max_new, a->b.max_len,
                                           a->paged != 0);
+  if (!fits(p, a->hkv)) return SAMKV_EUNSUPPORTED;
   if (!enough(ws, ws_bytes, p.bytes)) return SAMKV_EWORKSPACE;
   a->target_log2 = p.target_log2; a->ragged_log2 = p.ragged_log2; a->min_chunk = p.min_chunk; a->max_slots = p.max_slots; a->tile_rows = p.tile_rows;
   a->max_chunks = p.joins ? 0x7FFFFFFF : 1;
@@ -1046,7 +1049,8 @@ size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_l
                                      int32_t head_dim, int32_t dtype) {
   if (check_prompts(n_seq, n_tok, max_len, n_q_heads, n_kv_heads, head_dim, dtype) != SAMKV_OK) return 0;
   const int most = max_len < n_tok ? max_len : n_tok;
-  return paged_attn_plan(dtype, head_dim, n_q_heads, n_kv_heads, n_seq, n_tok, most, most, false).bytes;
+  const PagedAttnPlan p = paged_attn_plan(dtype, head_dim, n_q_heads, n_kv_heads, n_seq, n_tok, most, most, false);
+  return fits(p, n_kv_heads) ? p.bytes : 0;
 }
 
 int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_rows* v, const int32_t* cu, int32_t n_seq,
@@ -1067,6 +1071,7 @@ int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_row
   a.b.cu = cu;
   a.lse = lse; a.scale = scale;
   if ((rc = place_parts(&a, ws, ws_bytes)) != SAMKV_OK) return rc;
+  if (a.out.p == a.q.p || a.out.p == a.k.p || a.out.p == a.v.p) return SAMKV_EINVAL;  // rows are read after others are written
   return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -1099,8 +1104,9 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
 size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads) {
   BatchArg b;
   if (check_batch(pages, batch, n_q_heads, &b) != SAMKV_OK) return 0;
-  return paged_attn_plan(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new, b.max_len,
-                         true).bytes;
+  const PagedAttnPlan p = paged_attn_plan(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new,
+                                          b.max_len, true);
+  return fits(p, pages->n_kv_heads) ? p.bytes : 0;
 }
 
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
@@ -1119,6 +1125,7 @@ int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const s
   a.k.hs = a.v.hs = (long long)pages->page_size * d * e;
   a.lse = lse; a.scale = scale;
   if ((rc = place_parts(&a, ws, ws_bytes)) != SAMKV_OK) return rc;
+  if (a.out.p == a.q.p || a.out.p == a.k.p || a.out.p == a.v.p) return SAMKV_EINVAL;  // rows are read after others are written
   return dev(launch_paged_attn(a, static_cast<hipStream_t>(stream)));
 }
 
