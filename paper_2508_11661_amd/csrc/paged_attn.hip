@@ -681,6 +681,18 @@ static int prompt_shape(long long rows, long long mean_len, int max_len) {
 // 32 / 128 / 256 rows: 115 / 62 / 78; 2 x 512 over 8000: 264 / 138 / 153; 1 x 2048 over 16000: 953 / 508 / 486).
 static int paged_shape(long long most, long long rows) { return most <= 64 ? 0 : rows <= 49152 ? 2 : 1; }
 
+// Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share` of
+// the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the other
+// units save.  Where they all have one, only sequences of very different lengths gain, which the host does not see, and long ones
+// are cut so that none takes the time of many.  Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4 sequences of
+// 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to 2000 59 / 61, 375 to
+// 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 4 x 40 tokens over 1100 30.5 / 31.4, 1500 35.6 / 33.0, 1 x 500 over 2000 43 / 44, 3000
+// 50 / 46, 16 x 40 over 400 to 3000 52 / 56, 750 to 6000 89 / 93; 32 sequences, one of 30000 keys and the others of 500: 400 / 170.
+static bool cuts(int kg, double share, double passes) {
+  if (kg > 0) return passes > (share <= 0.5 ? 8 / (1 - share) : 32);
+  return passes > (share < 1 && 3 / (1 - share) < 16 ? 3 / (1 - share) : 16);
+}
+
 PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
@@ -688,13 +700,13 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv) : prompt_shape(rows * hkv, n_rows / n, max_len);
   p.once = most <= 32;
   p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
-  p.min_chunk = 256;
+  p.min_chunk = p.kg > 0 || (dtype == SAMKV_BF16 && d == 64) ? 256 : 128;  // four waves with a tile of keys each
   const long long wide = p.kg == 2 ? 128 : 256;
-  p.joins = paged && max_len > p.min_chunk;  // prompts have rows enough: the join would be one more launch
   // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-ragged_log2 of the keys that
   // the tiles of all heads see).
   const long long tile = p.kg > 0 ? wide : 32, with_rows = less(n, n_rows);  // sequences with rows
   const long long tiles = less(with_rows * ((most + tile - 1) / tile), rows / tile + with_rows);
+  p.joins = paged && cuts(p.kg, tiles * hkv / 256.0, (double)max_len / (p.kg > 0 ? 128 : p.min_chunk));
   p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? 10 : p.target_log2;  // fewer have many chunks each
   const long long shares = ((1 << p.ragged_log2) + hkv - 1) / hkv;
   p.max_items = (int)(tiles + (p.joins ? shares : 0));

@@ -69,8 +69,8 @@ struct Items {
     tiles = n_tiles(q);
   }
   __device__ __forceinline__ void count() {
-    const int c = is_wide(q) ? c_wide : c_few, per = is_wide(q) ? wide_rows<KG>() / 32 : 1;
-    chunks = a.max_chunks > 1 ? max((q.len + c - 1) / c, 1) : 1;
+    const int per = is_wide(q) ? wide_rows<KG>() / 32 : 1;
+    chunks = a.max_chunks > 1 ? max(is_wide(q) ? (q.len + c_wide / 4) / c_wide : (q.len + c_few - 1) / c_few, 1) : 1;
     slots = chunks > 1 ? tiles * chunks * per : 0;
     upto = scan64(JOIN ? (chunks > 1 ? tiles * per : 0) : tiles * chunks);
     slots_to = a.max_chunks > 1 ? scan64(slots) : 0;
@@ -100,7 +100,10 @@ struct Items {
       const int log2 = uneven ? a.ragged_log2 : a.target_log2;
       const int share = (int)min((total * a.hkv + (1ull << log2) - 1) >> log2, 0x40000000ull);
       c_few = max((share + 63) / 64 * 64, a.min_chunk);
-      c_wide = max((share / wide_cost<KG>() + 128) / 128 * 128, 2 * a.min_chunk);
+      // Wide tiles fill a compute unit and spend the time of 500 keys on their start and end: no more of them than there are units,
+      // so a sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 59 us
+      // with two chunks, 36 with one; 500 over 8000, 128 tiles: 87 with two, 113 with one).
+      c_wide = max(share / wide_cost<KG>(), 2 * a.min_chunk);
     }
     if (KG > 0 && a.paged && a.b.n_seq > 1 && a.b.n_seq <= 64) {
       int rank = 0;
