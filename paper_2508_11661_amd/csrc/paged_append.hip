@@ -5,7 +5,7 @@
 //
 // Many tokens: bound by HBM, 2 d e (2 Hkv + Hq) bytes per token read and written.  32 heads over 8, d = 128, bf16: 65536 tokens
 // 305 us, 5.28 TB/s, 4096 tokens 21 us (a copy of 2 GiB: 5.8 TB/s; float32, 32768 tokens: 318 us, 5.06).  A workgroup takes four
-// tokens of 4 KB / (d e) heads; one that walks all heads of its tokens, and so finds their angles once, is slower (315 us).
+// tokens of 4 KB / (d e) heads, or walks all their heads (run()).
 // Rows as (token, head) pairs in one list, so that few heads keep all lanes busy, lose what they gain: 306 us, 8 heads over 2 of
 // 64 channels 107 -> 125 us.  Non-temporal stores take 287 us, but the attention that reads the pages next pays more than that (8
 // sequences of 1024 tokens, both: 164 -> 167 us; 64: 1193 -> 1217).
@@ -31,17 +31,17 @@ __global__ __launch_bounds__(256) void k_paged_append(AppendLaunch a) {
   const int half = a.rot / 2;
 
   u32x4 x[TPB];
-  const int hh = blockIdx.y * RPB + rg;
-  {
-    const int h0 = min(hh, heads - 1);
-    const RowsArg& r = h0 < a.hq ? a.q : h0 < a.hq + a.hkv ? a.k_new : a.v_new;
-    const int head = h0 < a.hq ? h0 : h0 < a.hq + a.hkv ? h0 - a.hq : h0 - a.hq - a.hkv;
+  auto load = [&](int hh) {
+    const RowsArg& r = hh < a.hq ? a.q : hh < a.hq + a.hkv ? a.k_new : a.v_new;
+    const int head = hh < a.hq ? hh : hh < a.hq + a.hkv ? hh - a.hq : hh - a.hq - a.hkv;
 #pragma unroll
     for (int t = 0; t < TPB; ++t) {
       const int tok = min(tok0 + t, a.b.n_rows - 1);
       x[t] = *reinterpret_cast<const u32x4*>(r.p + head * r.hs + tok * r.rs + c * 16);
     }
-  }
+  };
+  int hh = blockIdx.y * RPB + rg;
+  load(min(hh, heads - 1));
 
   {
     const int tok = tok0 + wave;
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void k_paged_append(AppendLaunch a) {
   }
   __syncthreads();
 
-  if (hh < heads) {
+  for (; hh < heads; hh += gridDim.y * RPB) {
     const int kind = hh < a.hq ? 0 : hh < a.hq + a.hkv ? 1 : 2;  // query, key, value
     const int head = kind == 0 ? hh : kind == 1 ? hh - a.hq : hh - a.hq - a.hkv;
 #pragma unroll
@@ -128,6 +128,7 @@ __global__ __launch_bounds__(256) void k_paged_append(AppendLaunch a) {
       else to = s_at[t] >= 0 ? (kind == 1 ? a.k : a.v) + s_at[t] + ((long long)head << a.b.page_log2) * ROWB : nullptr;
       if (to != nullptr) *reinterpret_cast<u32x4*>(to + c * 16) = y;
     }
+    if (hh + (int)gridDim.y * RPB < heads) load(hh + gridDim.y * RPB);
   }
 }
 
@@ -136,7 +137,11 @@ hipError_t run(const AppendLaunch& a, hipStream_t s) {
   constexpr int RPB = 256 / (D / (BF16 ? 8 : 4));
   const int heads = a.hq + 2 * a.hkv, per = (heads + RPB - 1) / RPB;
   const unsigned n = (unsigned)((a.b.n_rows + TPB - 1) / TPB);
-  hipLaunchKernelGGL((k_paged_append<BF16, D>), dim3(n, per), dim3(256), 0, s, a);
+  // A workgroup per RPB heads, except where a quarter of its lanes or more would have no head and there are tokens enough: then one
+  // walks all heads of its tokens.  Spread / walked, us: 16384 tokens of 32 heads over 8, bf16, d = 128: 78.6 / 84.0, 2048: 10.8 / 12.7;
+  // 14 heads over 2 (18 rows for workgroups of 16), float32, d = 64: 16384 tokens 28.1 / 25.7, 6144 13.3 / 12.6, 2048 7.3 / 7.8.
+  const bool spread = n < 1024 || 4 * heads >= 3 * per * RPB;
+  hipLaunchKernelGGL((k_paged_append<BF16, D>), dim3(n, spread ? per : 1), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
