@@ -18,6 +18,9 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 // + NW, ...  Each wave has its own K and V slot in LDS, filled by asynchronous loads one tile ahead of their use (K of the next
 // tile is requested as soon as K's fragments are in registers, V likewise), so there is no barrier until the waves' results are
 // joined.
+// Bound by HBM while each key is read once: 64 sequences x 4096 keys, 32 heads over 8, d = 128: 163 us, 6.6 TB/s (reading 2 GiB: 7.1);
+// one of 131072 keys 86 + 5 us for the join, 6.0 TB/s.  Few short sequences are bound by the chain launch, lengths, page table, K, V,
+// join: 4 x 1000 keys 15 us with the append before it.
 template <int D, int NW>
 struct FewCfg {
   static constexpr int ROWB = D * 2, CPR = ROWB / 16, RPI = 1024 / ROWB;  // bytes and chunks per row, rows per request
@@ -232,6 +235,11 @@ __global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
 // KG = 1: 256 rows and 64 keys a step, tiles requested two steps ahead.  KG = 2, where 256 rows at a time would leave compute
 // units idle or the longest tile's chain of steps would last: 128 rows, and 128 keys a step of which either half of the waves
 // takes 64; the halves meet through LDS at the end.
+// Bound by the power limit: matrix and vector units are each busy half of the time, at 1.93 GHz.  One prompt of 24000
+// tokens, 32 heads over 8: d = 128 1116 TFLOP/s, d = 64 924; 16 of 1024 tokens 637: a workgroup's start and end (lengths, first K tile,
+// queries, output rows) take as long as four steps of a mean of 8.5.  Two workgroups of 128 rows and four waves per compute unit, whose
+// starts and ends overlap, read K and V twice as often: 16 x 1024 217 -> 203 us, but 23 of 580 to 2999 tokens 813 -> 817, 1 x 8000 498 ->
+// 514, chunks over pages up to 8 % slower.
 template <int D, int KG>
 struct WideCfg {
   static constexpr int NW = 8, RG = NW / KG, BK = 64, BKT = BK * KG;    // waves, row groups, keys per wave and per step
@@ -439,8 +447,8 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       }
       ++tile;
     };
-    // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The order of the instructions is fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier):
-    // a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
+    // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The order of the instructions is
+    // fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier): a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
     // use, and the maximum of the new scores under the last products.
     float mx = 0.f;
     auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto kind) {

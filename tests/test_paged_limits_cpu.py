@@ -17,9 +17,10 @@ def test_outputs_in_place_of_an_input_are_refused(S):  # noqa: F811
 
 @pytest.mark.parametrize("heads,n,size", [(65535, 128, -2), (4096, 128, -1)])
 def test_grids_beyond_32_bits_are_refused(S, heads, n, size):  # noqa: F811
-    """65535 heads of 128 sequences that may have 128 rows each are 129 * 65535 workgroups of 512 threads: more than 2^32 - 1.
-    4096 heads are fewer, and the next check, of out in place of q, answers."""
-    pages, batch = _pages(S, hkv=heads), _batch(S, n_seq=n, max_new=n, n_new=n, cu=FAKE, max_pages=100, max_len=1600)
+    """65535 heads of 128 sequences that may have 128 rows each are 128 * 65535 workgroups of 512 threads (65535 less than 2^32 - 1) and
+    one more per head where keys may be cut, as those of 16000 are.  4096 heads are fewer, and the next check, of out in place of
+    q, answers."""
+    pages, batch = _pages(S, hkv=heads), _batch(S, n_seq=n, max_new=n, n_new=n, cu=FAKE, max_pages=1000, max_len=16000)
     rows = _rows(S, hs=128, rs=128 * heads)
     assert S._lib.samkv_paged_attn(pages, batch, rows, heads, 0.1, rows, None, FAKE * 256, 1 << 50, None) == size
     assert (S._lib.samkv_paged_workspace_bytes(pages, batch, heads) > 0) == (size == -1)
