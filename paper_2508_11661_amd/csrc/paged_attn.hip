@@ -448,8 +448,9 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       ++tile;
     };
     // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The order of the instructions is
-    // fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier): a product every 32 cycles, between them two weights per two products, the fragment reads eight products ahead of their
-    // use, and the maximum of the new scores under the last products.
+    // fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier): a product every 32 cycles,
+    // between them two weights per two products, the fragment reads eight products ahead of their use, and the maximum of the
+    // new scores under the last products.
     float mx = 0.f;
     auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto kind) {
       constexpr bool masked = kind.value;
