@@ -684,11 +684,17 @@ static int prompt_shape(long long rows, long long mean_len, int max_len) {
   const double few = time(32, 512, 0.45, 0.7, 1.5), mid = time(128, 256, 0.5, 0.5, 4), wide = time(256, 256, 1, 1, 4);
   return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
 }
-// New tokens over a cache, whose keys are cut into chunks until the chip is full: tiles of 32 rows where no sequence has more than
-// two of them (8 sequences of 4000 keys, 32 heads over 8, 32-row / wide tiles, us: two 37.8 / 40.6, three 60 / 42; 32 of 2000, 8
-// heads over 2 of 64 channels: 24.5 / 28.2, 32.5 / 30.0), 128 rows where there are few of them (4 x 256 tokens over 3000, 32 heads,
-// 32 / 128 / 256 rows: 115 / 62 / 78; 2 x 512 over 8000: 264 / 138 / 153; 1 x 2048 over 16000: 953 / 508 / 486).
-static int paged_shape(long long most, long long rows) { return most <= 64 ? 0 : rows <= 49152 ? 2 : 1; }
+// New tokens over a cache: tiles of 32 rows where they are few (`tiles`, of all heads) and have few keys to see, since two of them
+// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256 rows,
+// us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 14.4 / 19.0 / 25.1, 4 x 128 20.1 / 20.3 / 26.5, 16 x 64 36 / 24 / 29, 64 x 40 85 / 82 /
+// 60; over 2000: 1 x 64 18.9 / 24.7 / 30, 4 x 40 34 / 31 / 34, 4 x 400 126 / 76 / 66; over 6000: 1 x 256 70 / 47 / 49; 8 heads over 2, d = 64: 4 x
+// 40 over 2000 14.6 / 21 / 24, 16 x 64 25 / 31 / 30, 16 x 200 49 / 29 / 45, 64 x 40 over 600 25 / 19 / 21.  Sequences of at most two such tiles
+// have less to gain from sharing keys: 64 x 16 over 600 39 / 46 / 47, over 2000 123 / 117 / 118, 16 x 16 over 6000 94 / 93 / 96.
+static int paged_shape(long long most, long long rows, int max_len, int d) {
+  const double tiles = rows / 32.0, keys = tiles * max_len;
+  if (most <= 64 ? keys <= 1.2e6 : tiles <= 512 && keys * d <= 2.7e5 * 128) return 0;
+  return rows <= 49152 ? 2 : 1;
+}
 
 // Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share` of
 // the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the other
@@ -706,7 +712,7 @@ PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int 
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
   auto less = [](long long x, long long y) { return x < y ? x : y; };
-  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv) : prompt_shape(rows * hkv, n_rows / n, max_len);
+  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv, max_len, d) : prompt_shape(rows * hkv, n_rows / n, max_len);
   p.once = most <= 32;
   p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
   p.min_chunk = p.kg > 0 || (dtype == SAMKV_BF16 && d == 64) ? 256 : 128;  // four waves with a tile of keys each

@@ -31,6 +31,17 @@ def test_pages(dtype, d, hq, hkv, page, lens, new):
     Paged(len(lens) + d, dtype, d, hq, hkv, page, lens, new).check(S, "tokens")
 
 
+@pytest.mark.parametrize("d,hq,hkv,page,lens,new", [
+    (128, 8, 2, 16, [400] * 6, [350] * 6), (64, 8, 2, 32, [400] * 6, [350] * 6),                       # more than 512 tiles of 32 rows
+    (128, 6, 2, 64, [300, 80] * 40, [100, 40] * 40), (64, 6, 2, 64, [300, 80] * 40, [100, 40] * 40),  # and more than 64 sequences
+    (128, 8, 2, 16, [6000, 5000, 300, 2], [60, 50, 100, 1]), (64, 8, 2, 16, [9000, 5000, 300, 2], [120, 100, 100, 1]),  # long ones
+    (128, 16, 1, 1024, [7000, 10], [100, 10]),
+])
+def test_pages_in_tiles_of_128_rows(d, hq, hkv, page, lens, new):
+    from paper_2508_11661_amd import samkv as S
+    Paged(sum(new) + d, "bf16", d, hq, hkv, page, lens, new, extra_rows=2).check(S, "tokens")
+
+
 @pytest.mark.parametrize("d,hq,hkv,lens", [
     (128, 32, 8, [700, 1, 300] + [30] * 70), (64, 32, 8, [700, 1, 300] + [30] * 70), (128, 32, 8, [520] * 6), (64, 32, 8, [520] * 12),
     (128, 16, 2, [1400]), (64, 16, 2, [2100]), (128, 5, 1, [257, 256, 255, 9, 8, 7]),
