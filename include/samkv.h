@@ -419,9 +419,8 @@ typedef struct {
  * one, which can make a call some hundred times slower).  out must not overlap q, k or v (the same address: SAMKV_EINVAL).
  * row_stride of k and v is below 2^24 bytes (SAMKV_EUNSUPPORTED).
  * Arithmetic: scores, maxima, sums and outputs are float32.  float32: products are float32.  bf16: products of bf16 values are
- * exact; a softmax weight enters its product with v rounded to 16 significant bits (two bf16 terms) where sequences are taken in
- * tiles of 32 rows, and to bf16 (2^-8 of its value at most, its sum over the keys being that of the unrounded weights) in wide
- * tiles; which those are follows from the bounds, not from the data.  Equal calls give equal bits.
+ * exact; a softmax weight enters its product with v rounded to 16 significant bits (two bf16 terms), its sum over the keys being
+ * that of the unrounded weights.  Equal calls give equal bits.
  * ws: samkv_prefill_workspace_bytes(...) bytes, 256-byte aligned; 0 bytes are needed today, and NULL is taken then. */
 size_t samkv_prefill_workspace_bytes(int32_t n_seq, int32_t n_tok, int32_t max_len, int32_t n_q_heads, int32_t n_kv_heads,
                                      int32_t head_dim, int32_t dtype);

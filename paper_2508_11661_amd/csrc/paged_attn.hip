@@ -230,16 +230,18 @@ __global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
 // so that the matrix unit and the vector unit work at the same time:
 //     step t:  S(t+1) = K(t+1) Q^T (matrix)  |  P(t) = 2^(S(t) c - m) (vector);  O^T += V(t)^T P(t)^T (matrix)
 // The running maximum is raised only when a row outgrows it by 2^8, which keeps the rescaling of O off the common path: weights
-// stay below 256.  They are rounded to bf16 (half a step, 2^-8 relative, as the output is in the end); their sum is that of the
-// unrounded weights, in float32.
+// stay below 256.  A weight is the sum of two bf16 terms (16 significant bits), each multiplied by V, as in attend_few: a token's
+// error is that of its output's rounding, whatever batch it comes in.  One term (half a step, 2^-8 relative) would take two matrix
+// products per key instead of three, 4.4 ms instead of 6.0 for 16 prompts of 4096 tokens, 64 heads over 8, but doubles the squared
+// error of the outputs (2.2e-3 of their norm instead of 1.6e-3).  The sum is that of the unrounded weights, in float32.
 // KG = 1: 256 rows and 64 keys a step, tiles requested two steps ahead.  KG = 2, where 256 rows at a time would leave compute
 // units idle or the longest tile's chain of steps would last: 128 rows, and 128 keys a step of which either half of the waves
 // takes 64; the halves meet through LDS at the end.
-// Bound by the power limit: matrix and vector units are each busy half of the time, at 1.93 GHz.  One prompt of 24000
-// tokens, 32 heads over 8: d = 128 1116 TFLOP/s, d = 64 924; 16 of 1024 tokens 637: a workgroup's start and end (lengths, first K tile,
-// queries, output rows) take as long as four steps of a mean of 8.5.  Two workgroups of 128 rows and four waves per compute unit, whose
-// starts and ends overlap, read K and V twice as often: 16 x 1024 217 -> 203 us, but 23 of 580 to 2999 tokens 813 -> 817, 1 x 8000 498 ->
-// 514, chunks over pages up to 8 % slower.
+// Bound by the power limit.  One prompt of 24000 tokens, 32 heads over 8: d = 128 780 TFLOP/s of the operator, 1170 of the matrix
+// unit; d = 64 630; 16 of 1024 tokens 510: a workgroup's start and end (lengths, first K tile, queries, output rows) take as long as
+// three steps of a mean of 8.5.  Measured with one-term weights: two workgroups of 128 rows and four waves per compute unit, whose starts
+// and ends overlap, read K and V twice as often: 16 x 1024 217 -> 203 us, but 23 of 580 to 2999 tokens 813 -> 817, 1 x 8000 498 -> 514,
+// chunks over pages up to 8 % slower.
 template <int D, int KG>
 struct WideCfg {
   static constexpr int NW = 8, RG = NW / KG, BK = 64, BKT = BK * KG;    // waves, row groups, keys per wave and per step
@@ -449,24 +451,25 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     };
     // S(tile) is in sc, its row maximum in mx; S(tile + 1) and its maximum take their places.  The order of the instructions is
     // fixed (a wave issues in order, and the two waves of a SIMD are in step after every barrier): a product every 32 cycles,
-    // between them two weights per two products, the fragment reads eight products ahead of their use, and the maximum of the
-    // new scores under the last products.
+    // between them the weights (a pair takes the vector unit for two products), the fragment reads eight products ahead of their
+    // use, and the maximum of the new scores under the last products.
     float mx = 0.f;
     auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto kind) {
       constexpr bool masked = kind.value;
-      constexpr int NS = 2 * ND, NP = 4 * NV;  // products of S and of O
+      constexpr int NS = 2 * ND, NP = 8 * NV, RV = 4;  // products of S and of O, fragments of V that are here
+      constexpr int FIRST = 4, UNDER_S = 4;    // pairs of weights made ahead of the products and under those of S
       uint32_t ks = k_at + s1, vs = v_at + s0;
       asm volatile("" : "+v"(ks), "+v"(vs));
-      bf16x8 ak[ND], bp[4];
-      Frag va[2 * NV];
+      bf16x8 ak[ND], hi[4], lo[4];
+      Frag va[RV];
       float psum = 0.f;
       auto k_read = [&](int i) {
         ak[i % ND] = *lds_at<bf16x8>((ks ^ ((i % ND) << 5)) + (i / ND) * 32 * ROWB);
       };
       auto v_read = [&](int j) {
         const uint32_t vp = (vs ^ ((j % NV) << 6)) + (j / NV) * 16 * ROWB;
-        va[j % (2 * NV)].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp));
-        va[j % (2 * NV)].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp + 8 * ROWB));
+        va[j % RV].s.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp));
+        va[j % RV].s.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(lds_at<s16x4>(vp + 8 * ROWB));
       };
 #pragma unroll
       for (int i = 0; i < ND; ++i) k_read(i);
@@ -476,13 +479,15 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         const int g = k / 4, e = 2 * (k % 4);
         const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e], c2, -m_use));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e + 1], c2, -m_use));
-        bp[g][e] = (__bf16)p0;
-        bp[g][e + 1] = (__bf16)p1;
+        hi[g][e] = (__bf16)p0;
+        hi[g][e + 1] = (__bf16)p1;
+        lo[g][e] = (__bf16)(p0 - (float)hi[g][e]);
+        lo[g][e + 1] = (__bf16)(p1 - (float)hi[g][e + 1]);
         psum += p0 + p1;
         asm volatile("" : : "v"(psum));  // here, not where the sum is used
       };
 #pragma unroll
-      for (int k = 0; k < 4; ++k) pair(k);
+      for (int k = 0; k < FIRST; ++k) pair(k);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
@@ -492,8 +497,8 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         }
         sn[i / ND] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ak[i % ND], bq[i % ND], sn[i / ND], 0, 0, 0);
         if (i < ND) k_read(i + ND);
-        else if (i - ND < 2 * NV) v_read(i - ND);
-        if ((i + 1) * 8 / NS > i * 8 / NS) pair(4 + i * 8 / NS);
+        else if (i - (NS - RV) >= 0) v_read(i - (NS - RV));
+        if ((i + 1) * UNDER_S / NS > i * UNDER_S / NS) pair(FIRST + i * UNDER_S / NS);
         if (i == NS / 4 && !masked) ahead_k();
         if (i == NS / 2 && !masked) ahead_v();
         __builtin_amdgcn_sched_barrier(0);
@@ -501,12 +506,12 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
       float top = -INFINITY;  // of the new scores
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
-        o[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[j % (2 * NV)].b, bp[j / NV], o[j % NV], 0, 0, 0);
-        if (j + 2 * NV < NP) v_read(j + 2 * NV);
-        constexpr int EARLY = NP / 4, PER = 4 / EARLY > 0 ? 4 / EARLY : 1, MAXES = (32 / (NP - EARLY) + 2) / 2 * 2;  // pairs: one instruction takes two
+        const int f = j / 2, g = f / NV;  // fragment of V, its 16 keys
+        o[f % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[f % RV].b, j % 2 == 0 ? hi[g] : lo[g], o[f % NV], 0, 0, 0);
+        if (j % 2 != 0 && f + RV < 4 * NV) v_read(f + RV);
+        constexpr int LATE = 16 - FIRST - UNDER_S, EARLY = NP / 2, MAXES = (32 / (NP - EARLY) + 2) / 2 * 2;  // maxima: one instruction takes two
         if (j < EARLY) {
-#pragma unroll
-          for (int k = 0; k < PER; ++k) pair(12 + j * PER + k);
+          if ((j + 1) * LATE / EARLY > j * LATE / EARLY) pair(FIRST + UNDER_S + j * LATE / EARLY);
         } else if constexpr (!masked) {
 #pragma unroll
           for (int k = 0; k < MAXES; ++k) {
@@ -668,41 +673,43 @@ hipError_t raise_limit() {
 
 }  // namespace
 
-// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2 us, 1.4 where the chip is not full),
-// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each, one and a half for
-// tiles of 32 rows, of which two share one.
+// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not full),
+// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the smaller),
+// one and a half for tiles of 32 rows, of which two share one.
 // Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, tiles of 32 / 128 / 256
-// rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 11 / 13 / 14, 1 x 1000 34 / 25 / 34, 1 x 2048 90 / 52 / 63, 1 x 4096 311 / 175 /
-// 157, 4 x 512 48 / 33 / 26, 32 x 64 30 / 22 / 15, 20 x 300 97 / 71 / 48; d = 64, 8 heads: 1 x 700 11 / 14 / 18, 1 x 2048 19 / 25 /
-// 38, 1 x 4096 50 / 42 / 68.
+// rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 15 / 16, 1 x 1000 36 / 31 / 44, 1 x 2048 97 / 68 / 85, 1 x 4096 315 / 231 /
+// 210, 4 x 512 49 / 38 / 33, 32 x 64 29 / 22 / 15, 20 x 300 102 / 82 / 58; d = 64, 8 heads: 1 x 1000 12 / 20 / 30, 1 x 2048 20 / 32 /
+// 51, 1 x 4096 50 / 58 / 96, 10 x 700 31 / 32 / 24.
 static int prompt_shape(long long rows, long long mean_len, int max_len) {
   const double longest = max_len / 64.0, mean = mean_len / 128.0;
   auto time = [&](double tile, double resident, double of_longest, double of_mean, double ends) {
     const double a = of_longest * longest + ends, b = rows / tile / resident * (of_mean * mean + ends);
     return a > b ? a : b;
   };
-  const double few = time(32, 512, 0.45, 0.7, 1.5), mid = time(128, 256, 0.5, 0.5, 4), wide = time(256, 256, 1, 1, 4);
+  const double few = time(32, 512, 0.45, 0.8, 1.5), mid = time(128, 256, 0.5, 0.7, 5), wide = time(256, 256, 1, 1, 4);
   return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
 }
 // New tokens over a cache: tiles of 32 rows where they are few (`tiles`, of all heads) and have few keys to see, since two of them
-// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256 rows,
-// us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 14.4 / 19.0 / 25.1, 4 x 128 20.1 / 20.3 / 26.5, 16 x 64 36 / 24 / 29, 64 x 40 85 / 82 /
-// 60; over 2000: 1 x 64 18.9 / 24.7 / 30, 4 x 40 34 / 31 / 34, 4 x 400 126 / 76 / 66; over 6000: 1 x 256 70 / 47 / 49; 8 heads over 2, d = 64: 4 x
-// 40 over 2000 14.6 / 21 / 24, 16 x 64 25 / 31 / 30, 16 x 200 49 / 29 / 45, 64 x 40 over 600 25 / 19 / 21.  Sequences of at most two such tiles
-// have less to gain from sharing keys: 64 x 16 over 600 39 / 46 / 47, over 2000 123 / 117 / 118, 16 x 16 over 6000 94 / 93 / 96.
+// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256
+// rows, us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 14.7 / 21.2 / 29.9, 4 x 128 19.4 / 22.7 / 30.3, 16 x 64 36 / 26
+// / 33, 64 x 40 78 / 93 / 69; over 2000: 1 x 64 19.5 / 28.0 / 34, 4 x 128 42 / 48 / 50, 4 x 400 118 / 93 / 83; over 6000: 1 x 64 32
+// / 37 / 49, 1 x 256 69 / 55 / 57; 8 heads over 2, d = 64: 4 x 400 over 2000 28 / 34 / 34, 16 x 64 24 / 31 / 34, 16 x 200 51 / 39 /
+// 60, over 6000: 4 x 400 73 / 60 / 59.  Sequences of at most two tiles of 32 have less to gain from sharing keys, 32 heads over 8,
+// d = 128: 64 x 16 over 600 39 / 50 / 50, over 2000 123 / 129 / 129, over 6000 309 / 303 / 303, 16 x 16 over 6000 90 / 95 / 95.
 static int paged_shape(long long most, long long rows, int max_len, int d) {
   const double tiles = rows / 32.0, keys = tiles * max_len;
-  if (most <= 64 ? keys <= 1.2e6 : tiles <= 512 && keys * d <= 2.7e5 * 128) return 0;
+  if (most <= 64 ? keys <= 2.6e6 : tiles <= 512 && keys * d <= 8e5 * 128) return 0;
   return rows <= 49152 ? 2 : 1;
 }
 
-// Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share` of
-// the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the other
-// units save.  Where they all have one, only sequences of very different lengths gain, which the host does not see, and long ones
-// are cut so that none takes the time of many.  Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4 sequences of
-// 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to 2000 59 / 61, 375 to
-// 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 4 x 40 tokens over 1100 30.5 / 31.4, 1500 35.6 / 33.0, 1 x 500 over 2000 43 / 44, 3000
-// 50 / 46, 16 x 40 over 400 to 3000 52 / 56, 750 to 6000 89 / 93; 32 sequences, one of 30000 keys and the others of 500: 400 / 170.
+// Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share`
+// of the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the
+// other units save.  Where they all have one, only sequences of very different lengths gain, which the host does not see, and long
+// ones are cut so that none takes the time of many.  Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4
+// sequences of 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to
+// 2000 59 / 61, 375 to 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 2 x 300 tokens over 1500 39.0 / 43.7, 8 x 200 over 3000 118
+// / 127, 1 x 500 over 2000 47.5 / 46.5, 3000 63 / 56, 8000 151 / 110, 16 x 64 over 400 to 3000 69 / 72, 750 to 6000 124 / 114; 32 x
+// 100, one over 30000 keys and the others over 600: 950 / 171.
 static bool cuts(int kg, double share, double passes) {
   if (kg > 0) return passes > (share <= 0.5 ? 8 / (1 - share) : 32);
   return passes > (share < 1 && 3 / (1 - share) < 16 ? 3 / (1 - share) : 16);

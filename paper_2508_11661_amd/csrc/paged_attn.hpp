@@ -44,10 +44,11 @@ struct Item {
 };
 
 // Finds work items: JOIN = false, number `index` of them; JOIN = true, group of 32 rows number `index` among the tiles whose keys
-// are cut (the chunk is the first).  All calls are by whole waves, and the results are the same in every lane.  A lane holds one
-// of 64 sequences; batches of up to that many are read once, and over a cache wide tiles are taken in order of falling length, so
-// that a long sequence's are not the last to start (24 sequences, three of them with 1024 new tokens: 447 -> 437 us; prompts gain
-// less than the order costs, 2 %).  Within a sequence items run chunk by chunk, the last tile (with the most keys) first.
+// are cut (the chunk is the first).  All calls are by whole waves, and the results are the same in every lane.  A lane holds one of
+// 64 sequences; batches of up to that many are read once, and over a cache wide tiles are taken in order of falling length, so that
+// a long sequence's are not the last to start (24 sequences with 1 to 1024 new tokens, those with many in front: 549 us either way,
+// at the end: 610 -> 520; prompts gain less than the order costs, 2 %).  Within a sequence items run chunk by chunk, the last tile
+// (with the most keys) first.
 template <int KG, bool JOIN>
 struct Items {
   const PagedAttnLaunch& a;
@@ -101,8 +102,8 @@ struct Items {
       const int share = (int)min((total * a.hkv + (1ull << log2) - 1) >> log2, 0x40000000ull);
       c_few = max((share + 63) / 64 * 64, a.min_chunk);
       // Wide tiles fill a compute unit and spend the time of 500 keys on their start and end: no more of them than there are units,
-      // so a sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 59 us
-      // with two chunks, 36 with one; 500 over 8000, 128 tiles: 87 with two, 113 with one).
+      // so a sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 62 us
+      // with chunks rounded up, 46 to the nearest, 42 uncut; 500 over 8000, 128 tiles: 118 either way, 151 uncut).
       c_wide = max(share / wide_cost<KG>(), 2 * a.min_chunk);
     }
     if (KG > 0 && a.paged && a.b.n_seq > 1 && a.b.n_seq <= 64) {
