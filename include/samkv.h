@@ -432,7 +432,8 @@ int samkv_prefill_attn(const samkv_rows* q, const samkv_rows* k, const samkv_row
  *   k_new, v_new  n_kv_heads of n_new rows, in the pages' dtype
  *   rope          NULL: nothing is rotated (keys that come rotated, as a compacted cache's do)
  *   q, q_out      n_q_heads of n_new rows, in the pages' dtype, q_out = q rotated; both NULL: no queries.  q_out may be q
- *                 itself (same address and strides); otherwise what is written must not overlap what is read.
+ *                 itself (same address and strides); otherwise what is written must not overlap what is read (the
+ *                 address of q with other strides, of k_new or of v_new: SAMKV_EINVAL).
  * Angles are reduced in float64, the rotation is float32 and rounded once.  A token without a slot, or whose page number is
  * outside [0, n_pages), is not written (its query still is rotated, by its given position, or else by 0).  Tokens that are
  * written to the same row of a page (of a page that two sequences share, say) leave a mixture of theirs there. */
