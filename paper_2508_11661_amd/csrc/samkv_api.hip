@@ -1089,15 +1089,16 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
     if ((rc = check_rows(q, n_q_heads, n, d, dtype, false, &a.q)) != SAMKV_OK) return rc;
     if ((rc = check_rows(q_out, n_q_heads, n, d, dtype, true, &a.q_out)) != SAMKV_OK) return rc;
     a.hq = n_q_heads;
-    // rows are read after others are written: only in place, every row where it is read
-    const bool in_place = (n_q_heads == 1 || a.q.hs == a.q_out.hs) && (n == 1 || a.q.rs == a.q_out.rs);
-    if (a.q_out.p == a.k_new.p || a.q_out.p == a.v_new.p || (a.q_out.p == a.q.p && !in_place)) return SAMKV_EINVAL;
   }
   if (rope != nullptr) {
     if (rope->inv_freq == nullptr || (uintptr_t)rope->inv_freq % 4 != 0 || (uintptr_t)rope->positions % 4 != 0) return SAMKV_EINVAL;
     if (rope->rot_dim < 1 || rope->rot_dim > d || rope->rot_dim % 2 != 0) return SAMKV_EINVAL;
     if (rope->rot_dim % 16 != 0) return SAMKV_EUNSUPPORTED;
     a.inv_freq = rope->inv_freq; a.rot = rope->rot_dim; a.interleaved = rope->interleaved != 0; a.positions = rope->positions;
+  }
+  if (with_q) {  // rows are read after others are written: only in place, every row where it is read
+    const bool in_place = (n_q_heads == 1 || a.q.hs == a.q_out.hs) && (n == 1 || a.q.rs == a.q_out.rs);
+    if (a.q_out.p == a.k_new.p || a.q_out.p == a.v_new.p || (a.q_out.p == a.q.p && !in_place)) return SAMKV_EINVAL;
   }
   a.dtype = dtype; a.d = d; a.hkv = pages->n_kv_heads;
   a.k = static_cast<char*>(pages->k); a.v = static_cast<char*>(pages->v);
