@@ -3,6 +3,7 @@
 // nothing that they hold leads an access out of the tensors.
 #pragma once
 #include "common.hpp"
+#include "paged_plan.hpp"
 
 namespace samkv {
 
@@ -81,15 +82,5 @@ struct PagedAttnLaunch {
   float* part_lse;        // [max_slots][hkv][tile_rows], in units of log 2
 };
 hipError_t launch_paged_attn(const PagedAttnLaunch& a, hipStream_t s);
-
-// Sizes of a launch that follow from the bounds alone.
-struct PagedAttnPlan {
-  int kg;     // which wide tiles there are: see paged_attn.hpp
-  bool once;  // every sequence is one tile of 32 rows
-  int target_log2, ragged_log2, min_chunk, max_items, max_slots, tile_rows;
-  bool joins;  // whether any sequence can have more than one chunk
-  size_t part_lse, bytes;  // workspace: part_o, then part_lse
-};
-PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged);
 
 }  // namespace samkv

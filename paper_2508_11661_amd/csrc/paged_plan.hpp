@@ -1,0 +1,87 @@
+// Which kernels an attention over packed prompts or pages takes, and how large its grids and its workspace are: host arithmetic on the
+// bounds of a batch, without any HIP, so that a host compiler can build it alone.
+#pragma once
+#include <stddef.h>
+
+#include "../../include/samkv.h"
+
+namespace samkv {
+
+// Sizes of a launch that follow from the bounds alone.
+struct PagedAttnPlan {
+  int kg;     // which wide tiles there are: see paged_attn.hpp
+  bool once;  // every sequence is one tile of 32 rows
+  int target_log2, ragged_log2, min_chunk, max_items, max_slots, tile_rows;
+  bool joins;  // whether any sequence can have more than one chunk
+  size_t part_lse, bytes;  // workspace: part_o, then part_lse
+};
+
+// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not full),
+// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the smaller),
+// one and a half for tiles of 32 rows, of which two share one.
+// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, tiles of 32 / 128 / 256
+// rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 15 / 16, 1 x 1000 36 / 31 / 44, 1 x 2048 97 / 68 / 85, 1 x 4096 315 / 231 /
+// 210, 4 x 512 49 / 38 / 33, 32 x 64 29 / 22 / 15, 20 x 300 102 / 82 / 58; d = 64, 8 heads: 1 x 1000 12 / 20 / 30, 1 x 2048 20 / 32 /
+// 51, 1 x 4096 50 / 58 / 96, 10 x 700 31 / 32 / 24.
+inline int prompt_shape(long long rows, long long mean_len, int max_len) {
+  const double longest = max_len / 64.0, mean = mean_len / 128.0;
+  auto time = [&](double tile, double resident, double of_longest, double of_mean, double ends) {
+    const double a = of_longest * longest + ends, b = rows / tile / resident * (of_mean * mean + ends);
+    return a > b ? a : b;
+  };
+  const double few = time(32, 512, 0.45, 0.8, 1.5), mid = time(128, 256, 0.5, 0.7, 5), wide = time(256, 256, 1, 1, 4);
+  return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
+}
+// New tokens over a cache: tiles of 32 rows where they are few (`tiles`, of all heads) and have few keys to see, since two of them
+// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256
+// rows, us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 14.7 / 21.2 / 29.9, 4 x 128 19.4 / 22.7 / 30.3, 16 x 64 36 / 26
+// / 33, 64 x 40 78 / 93 / 69; over 2000: 1 x 64 19.5 / 28.0 / 34, 4 x 128 42 / 48 / 50, 4 x 400 118 / 93 / 83; over 6000: 1 x 64 32
+// / 37 / 49, 1 x 256 69 / 55 / 57; 8 heads over 2, d = 64: 4 x 400 over 2000 28 / 34 / 34, 16 x 64 24 / 31 / 34, 16 x 200 51 / 39 /
+// 60, over 6000: 4 x 400 73 / 60 / 59.  Sequences of at most two tiles of 32 have less to gain from sharing keys, 32 heads over 8,
+// d = 128: 64 x 16 over 600 39 / 50 / 50, over 2000 123 / 129 / 129, over 6000 309 / 303 / 303, 16 x 16 over 6000 90 / 95 / 95.
+inline int paged_shape(long long most, long long rows, int max_len, int d) {
+  const double tiles = rows / 32.0, keys = tiles * max_len;
+  if (most <= 64 ? keys <= 2.6e6 : tiles <= 512 && keys * d <= 8e5 * 128) return 0;
+  return rows <= 49152 ? 2 : 1;
+}
+
+// Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share`
+// of the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the
+// other units save.  Where they all have one, only sequences of very different lengths gain, which the host does not see, and long
+// ones are cut so that none takes the time of many.  Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4
+// sequences of 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to
+// 2000 59 / 61, 375 to 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 2 x 300 tokens over 1500 39.0 / 43.7, 8 x 200 over 3000 118
+// / 127, 1 x 500 over 2000 47.5 / 46.5, 3000 63 / 56, 8000 151 / 110, 16 x 64 over 400 to 3000 69 / 72, 750 to 6000 124 / 114; 32 x
+// 100, one over 30000 keys and the others over 600: 950 / 171.
+inline bool cuts(int kg, double share, double passes) {
+  if (kg > 0) return passes > (share <= 0.5 ? 8 / (1 - share) : 32);
+  return passes > (share < 1 && 3 / (1 - share) < 16 ? 3 / (1 - share) : 16);
+}
+
+inline PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
+  PagedAttnPlan p;
+  const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
+  auto less = [](long long x, long long y) { return x < y ? x : y; };
+  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv, max_len, d) : prompt_shape(rows * hkv, n_rows / n, max_len);
+  p.once = most <= 32;
+  p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
+  p.min_chunk = p.kg > 0 || (dtype == SAMKV_BF16 && d == 64) ? 256 : 128;  // four waves with a tile of keys each
+  const long long wide = p.kg == 2 ? 128 : 256;
+  // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-ragged_log2 of the keys that
+  // the tiles of all heads see).
+  const long long tile = p.kg > 0 ? wide : 32, with_rows = less(n, n_rows);  // sequences with rows
+  const long long tiles = less(with_rows * ((most + tile - 1) / tile), rows / tile + with_rows);
+  p.joins = paged && cuts(p.kg, tiles * hkv / 256.0, (double)max_len / (p.kg > 0 ? 128 : p.min_chunk));
+  p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? 10 : p.target_log2;  // fewer have many chunks each
+  const long long shares = ((1 << p.ragged_log2) + hkv - 1) / hkv;
+  p.max_items = (int)(tiles + (p.joins ? shares : 0));
+  // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
+  p.max_slots = (int)(p.joins ? less(p.max_items, 2 * shares) * (tile / 32) : 0);
+  p.tile_rows = (int)less(32, most);
+  const size_t part_rows = (size_t)p.max_slots * hkv * p.tile_rows;
+  p.part_lse = (part_rows * d * 4 + 255) / 256 * 256;
+  p.bytes = p.part_lse + (part_rows * 4 + 255) / 256 * 256;
+  return p;
+}
+
+}  // namespace samkv
