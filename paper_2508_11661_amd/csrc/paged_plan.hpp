@@ -58,30 +58,57 @@ inline bool cuts(int kg, double share, double passes) {
   return passes > (share < 1 && 3 / (1 - share) < 16 ? 3 / (1 - share) : 16);
 }
 
+// Tiles of `tile` rows that there can be: sequences have at most `most` rows per KV head and `rows` together.
+inline long long tiles_of(long long n_seq, long long n_rows, long long rows, long long most, long long tile) {
+  const long long with_rows = n_seq < n_rows ? n_seq : n_rows;  // sequences with rows
+  const long long each = with_rows * ((most + tile - 1) / tile), packed = rows / tile + with_rows;
+  return each < packed ? each : packed;
+}
+inline long long shares_of(int log2, int hkv) { return ((1 << log2) + hkv - 1) / hkv; }
+// Only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
+inline long long slots_of(long long tiles, long long shares, long long tile) {
+  return (tiles + shares < 2 * shares ? tiles + shares : 2 * shares) * (tile / 32);
+}
+constexpr int kUneven = 10;  // target_log2 and ragged_log2 of tiles of 32 rows: at most
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
 inline PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
-  auto less = [](long long x, long long y) { return x < y ? x : y; };
   p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv, max_len, d) : prompt_shape(rows * hkv, n_rows / n, max_len);
   p.once = most <= 32;
   p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
   p.min_chunk = p.kg > 0 || (dtype == SAMKV_BF16 && d == 64) ? 256 : 128;  // four waves with a tile of keys each
-  const long long wide = p.kg == 2 ? 128 : 256;
   // Items: the tiles that there can be, and the chunks that Items cuts (one holds at least 2^-ragged_log2 of the keys that
   // the tiles of all heads see).
-  const long long tile = p.kg > 0 ? wide : 32, with_rows = less(n, n_rows);  // sequences with rows
-  const long long tiles = less(with_rows * ((most + tile - 1) / tile), rows / tile + with_rows);
+  const long long tile = p.kg == 2 ? 128 : p.kg == 1 ? 256 : 32, tiles = tiles_of(n, n_rows, rows, most, tile);
   p.joins = paged && cuts(p.kg, tiles * hkv / 256.0, (double)max_len / (p.kg > 0 ? 128 : p.min_chunk));
-  p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? 10 : p.target_log2;  // fewer have many chunks each
-  const long long shares = ((1 << p.ragged_log2) + hkv - 1) / hkv;
+  p.ragged_log2 = p.kg == 0 && n > 1 && tiles * hkv >= 128 ? kUneven : p.target_log2;  // fewer have many chunks each
+  const long long shares = shares_of(p.ragged_log2, hkv);
   p.max_items = (int)(tiles + (p.joins ? shares : 0));
-  // Slots: only tiles of more than one chunk have partial results, and those have less than twice their share of chunks.
-  p.max_slots = (int)(p.joins ? less(p.max_items, 2 * shares) * (tile / 32) : 0);
-  p.tile_rows = (int)less(32, most);
+  p.max_slots = (int)(p.joins ? slots_of(tiles, shares, tile) : 0);
+  p.tile_rows = (int)(most < 32 ? most : 32);
   const size_t part_rows = (size_t)p.max_slots * hkv * p.tile_rows;
-  p.part_lse = (part_rows * d * 4 + 255) / 256 * 256;
-  p.bytes = p.part_lse + (part_rows * 4 + 255) / 256 * 256;
+  p.part_lse = up256(part_rows * d * 4);
+  p.bytes = p.part_lse + up256(part_rows * 4);
   return p;
+}
+
+// Workspace of an attention over pages: enough for every batch of the same heads whose counts and bounds are no larger, one of which may
+// be cut where this one is not (64 single tokens over 2048 keys are not, 4 are), or take smaller tiles.  The slots of either
+// kind of tiles grow with the bounds; a batch of one tile is the first to be cut.
+inline size_t paged_attn_workspace(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len) {
+  const PagedAttnPlan p = paged_attn_plan(dtype, d, hq, hkv, n_seq, n_rows, max_new, max_len, true);
+  const long long group = hq / hkv, rows = n_rows * group, most = max_new * group;
+  auto bytes = [&](int kg, int min_step, long long tile, int log2) -> size_t {
+    if (!cuts(kg, hkv / 256.0, (double)max_len / min_step)) return 0;
+    const size_t part_rows = (size_t)slots_of(tiles_of(n_seq, n_rows, rows, most, tile), shares_of(log2, hkv), tile) * hkv * (most < 32 ? most : 32);
+    return up256(part_rows * d * 4) + up256(part_rows * 4);
+  };
+  const bool even = n_seq == 1 || tiles_of(n_seq, n_rows, rows, most, 32) * hkv < 128;
+  const size_t few = bytes(0, dtype == SAMKV_BF16 && d == 64 ? 256 : 128, 32, even ? 9 : kUneven);
+  const size_t wide = p.kg > 0 ? bytes(p.kg, 128, p.kg == 2 ? 128 : 256, 8) : 0;  // a smaller batch takes no wider tiles
+  return few > wide ? few : wide;
 }
 
 }  // namespace samkv

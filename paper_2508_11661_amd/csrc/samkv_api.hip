@@ -1110,7 +1110,8 @@ size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* 
   if (check_batch(pages, batch, n_q_heads, &b) != SAMKV_OK) return 0;
   const PagedAttnPlan p = paged_attn_plan(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new,
                                           b.max_len, true);
-  return fits(p, pages->n_kv_heads) ? p.bytes : 0;
+  if (!fits(p, pages->n_kv_heads)) return 0;
+  return paged_attn_workspace(pages->dtype, pages->head_dim, n_q_heads, pages->n_kv_heads, b.n_seq, b.n_rows, b.max_new, b.max_len);
 }
 
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,

@@ -623,6 +623,7 @@ def samkv_paged_append(cache: PagedCache, batch: PagedBatch, k_new: torch.Tensor
 
 
 def samkv_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_q_heads: int) -> int:
+    """Enough for this batch and every one with no more sequences and tokens and no larger bounds."""
     return int(_lib.samkv_paged_workspace_bytes(cache.c, batch.c, n_q_heads))
 
 
