@@ -369,8 +369,8 @@ int samkv_kv_update(void* k_c, void* v_c, const void* k_new, const void* v_new, 
  *     page numbers outside [0, n_pages) are taken as the nearest page when they are read and not written to at all.
  *     Sequences are packed one behind the other; rows behind the last one are not written (and what they hold reaches
  *     nothing);
- *   - counts and bounds are at least 1 (SAMKV_EINVAL).  n_q_heads * rows is at most 2^23 - 1, a grid at most 2^32 - 1 threads
- *     (SAMKV_EUNSUPPORTED).
+ *   - counts and bounds are at least 1 (SAMKV_EINVAL).  n_q_heads * rows is at most 2^27 - 1, a grid at most 2^32 - 1 threads
+ *     (SAMKV_EUNSUPPORTED; of an append that is 2^26 - 4 tokens).
  * A device's first attention call (of these or of those above) sets up its kernels and must not be captured into a graph. */
 #define SAMKV_MAX_SEQ 4096
 typedef struct {
@@ -449,7 +449,7 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
  * Arithmetic as in samkv_prefill_attn; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long sequences are
  * cut into chunks whose results are joined in float32; which chunks there are follows from the lengths alone.
  * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned; that is enough for every batch of the same pages and heads whose n_seq,
- * n_new, max_new and max_len are no larger, so that a program allocates once for its largest batch (68 MB at most). */
+ * n_new, max_new and max_len are no larger, so that a program allocates once for its largest batch (68 MB at most for 8 KV heads of 128, some 110 MB for any). */
 size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads);
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
                      const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream);

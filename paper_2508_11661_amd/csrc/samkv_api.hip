@@ -972,6 +972,9 @@ int samkv_kv_update(void* k_c, void* v_c, const void* k_new, const void* v_new, 
 
 // ---- packed prompts and paged caches ----
 
+// Heads times rows: numbers of rows and tiles, and a grid's threads (16 per row at most), are 32-bit.
+constexpr long long kMaxQueryRows = (1 << 27) - 1;
+
 // Rows of `heads` heads that a kernel reads or writes (`written`: no two of them may share memory).
 static int check_rows(const samkv_rows* r, int heads, int rows, int d, int dtype, bool written, RowsArg* out) {
   if (r == nullptr || r->p == nullptr || !aligned16(r->p)) return SAMKV_EINVAL;
@@ -1011,7 +1014,7 @@ static int check_batch(const samkv_pages* pages, const samkv_batch* batch, int h
   if (batch->n_seq < 1 || batch->max_pages < 1 || batch->max_len < 1 || batch->max_new < 1 || batch->n_new < 1) return SAMKV_EINVAL;
   if (batch->max_len > (long long)batch->max_pages * size) return SAMKV_EINVAL;
   if (batch->cu_new == nullptr && (long long)batch->n_seq * batch->max_new != batch->n_new) return SAMKV_EINVAL;
-  if (batch->n_seq > SAMKV_MAX_SEQ || batch->max_len > 0x7FFFFFFF / 4 || (long long)hq * batch->n_new > 0x7FFFFFFF / 256)
+  if (batch->n_seq > SAMKV_MAX_SEQ || batch->max_len > 0x7FFFFFFF / 4 || (long long)hq * batch->n_new > kMaxQueryRows)
     return SAMKV_EUNSUPPORTED;
   b->n_seq = batch->n_seq; b->n_rows = batch->n_new; b->max_len = batch->max_len;
   b->max_new = batch->max_new < batch->n_new ? batch->max_new : batch->n_new;
@@ -1025,7 +1028,7 @@ static int check_prompts(int n_seq, int n_tok, int max_len, int hq, int hkv, int
   const int rc = check_heads(hq, hkv, d, dtype);
   if (rc != SAMKV_OK) return rc;
   if (n_seq < 1 || n_tok < 1 || max_len < 1) return SAMKV_EINVAL;
-  return n_seq > SAMKV_MAX_SEQ || (long long)hq * n_tok > 0x7FFFFFFF / 256 ? SAMKV_EUNSUPPORTED : SAMKV_OK;
+  return n_seq > SAMKV_MAX_SEQ || (long long)hq * n_tok > kMaxQueryRows ? SAMKV_EUNSUPPORTED : SAMKV_OK;
 }
 
 static bool fits(const PagedAttnPlan& p, int hkv) { return (long long)p.max_items * hkv * 512 <= 0xFFFFFFFFll; }  // threads of a grid
@@ -1083,6 +1086,7 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
   int rc = check_batch(pages, batch, with_q ? n_q_heads : pages != nullptr ? pages->n_kv_heads : 0, &a.b);
   if (rc != SAMKV_OK) return rc;
   const int d = pages->head_dim, dtype = pages->dtype, n = batch->n_new;
+  if (n > (1 << 26) - 4) return SAMKV_EUNSUPPORTED;  // a workgroup of 256 threads per four tokens
   if ((rc = check_rows(k_new, pages->n_kv_heads, n, d, dtype, false, &a.k_new)) != SAMKV_OK) return rc;
   if ((rc = check_rows(v_new, pages->n_kv_heads, n, d, dtype, false, &a.v_new)) != SAMKV_OK) return rc;
   if (with_q) {
