@@ -477,9 +477,11 @@ hipError_t launch_join(const PagedAttnLaunch& a, const PagedAttnPlan& p, hipStre
   // a tile that is cut has two slots at least; no more workgroups than are resident at once
   const long long rows = (long long)(p.max_slots / 2) * a.hkv * p.tile_rows;
   const dim3 grid((unsigned)(rows < 1536 ? rows : 1536));
-  if (p.kg == 2) hipLaunchKernelGGL((k_join_chunks<D, BF16, 2>), grid, dim3(256), 0, s, a);
-  else if (p.kg == 1) hipLaunchKernelGGL((k_join_chunks<D, BF16, 1>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_join_chunks<D, BF16, 0>), grid, dim3(256), 0, s, a);
+  if constexpr (BF16) {  // float32 has no wide tiles
+    if (p.kg == 2) hipLaunchKernelGGL((k_join_chunks<D, true, 2>), grid, dim3(256), 0, s, a);
+    if (p.kg == 1) hipLaunchKernelGGL((k_join_chunks<D, true, 1>), grid, dim3(256), 0, s, a);
+  }
+  if (p.kg == 0) hipLaunchKernelGGL((k_join_chunks<D, BF16, 0>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
