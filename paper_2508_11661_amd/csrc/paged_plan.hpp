@@ -16,21 +16,34 @@ struct PagedAttnPlan {
   size_t part_lse, bytes;  // workspace: part_o, then part_lse
 };
 
-// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not full),
-// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the smaller),
-// one and a half for tiles of 32 rows, of which two share one.
-// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, tiles of 32 / 128 / 256
-// rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 15 / 16, 1 x 1000 36 / 31 / 44, 1 x 2048 97 / 68 / 85, 1 x 4096 315 / 231 /
-// 210, 4 x 512 49 / 38 / 33, 32 x 64 29 / 22 / 15, 20 x 300 102 / 82 / 58; d = 64, 8 heads: 1 x 1000 12 / 20 / 30, 1 x 2048 20 / 32 /
-// 51, 1 x 4096 50 / 58 / 96, 10 x 700 31 / 32 / 24.
-inline int prompt_shape(long long rows, long long mean_len, int max_len) {
-  const double longest = max_len / 64.0, mean = mean_len / 128.0;
-  auto time = [&](double tile, double resident, double of_longest, double of_mean, double ends) {
-    const double a = of_longest * longest + ends, b = rows / tile / resident * (of_mean * mean + ends);
-    return a > b ? a : b;
+// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not
+// full), with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the
+// smaller), one and a half for tiles of 32 rows, of which two share one.
+// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, prompts of one length,
+// tiles of 32 / 128 / 256 rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 15 / 16, 1 x 1000 36 / 31 / 44, 1 x 2048 97 / 68
+// / 85, 1 x 4096 315 / 231 / 210, 4 x 512 49 / 38 / 33, 32 x 64 29 / 22 / 15, 20 x 300 102 / 82 / 58; d = 64, 8 heads: 1 x 1000 12
+// / 20 / 30, 1 x 2048 20 / 32 / 51, 1 x 4096 50 / 58 / 96, 10 x 700 31 / 32 / 24.
+// How the rows are spread over the sequences is known to the device alone: anything from evenly over all of them to prompts of
+// max_len beside sequences of padding (a captured batch with room for many), so the tiles are taken whose loss is smallest where it
+// is largest.  32 heads over 8, d = 128, 32 / 128 / 256 rows, us: 1 x 4000 tokens beside 70 x 30 363 / 277 / 237, 1 x 8192 and 511
+// sequences without rows 1108 / 857 / 798, 4 x 1024 and 60 without 112 / 78 / 79; 8 heads over 2: 83 / 81 / 130, 280 / 221 / 282,
+// 37 / 29 / 42.
+inline int prompt_shape(long long rows, long long n_rows, long long n_seq, int max_len) {
+  struct Times { double few, wide, mid; };
+  auto times = [&](double mean_len) {
+    const double longest = max_len / 64.0, mean = mean_len / 128;
+    auto time = [&](double tile, double resident, double of_longest, double of_mean, double ends) {
+      const double a = of_longest * longest + ends, b = rows / tile / resident * (of_mean * mean + ends);
+      return a > b ? a : b;
+    };
+    const Times t = {time(32, 512, 0.45, 0.8, 1.5), time(256, 256, 1, 1, 4), time(128, 256, 0.5, 0.7, 5)};
+    const double some = t.wide < t.mid ? t.wide : t.mid, best = t.few < some ? t.few : some;
+    return Times{t.few / best, t.wide / best, t.mid / best};
   };
-  const double few = time(32, 512, 0.45, 0.8, 1.5), mid = time(128, 256, 0.5, 0.7, 5), wide = time(256, 256, 1, 1, 4);
-  return few < mid && few < wide ? 0 : mid < wide ? 2 : 1;
+  const Times even = times(n_rows < n_seq ? 1 : n_rows / n_seq), packed = times(max_len < n_rows ? max_len : n_rows);
+  auto larger = [](double x, double y) { return x > y ? x : y; };
+  const double few = larger(even.few, packed.few), wide = larger(even.wide, packed.wide), mid = larger(even.mid, packed.mid);
+  return few <= wide && few <= mid ? 0 : wide <= mid ? 1 : 2;
 }
 // New tokens over a cache: tiles of 32 rows where they are few (`tiles`, of all heads) and have few keys to see, since two of them
 // share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256
@@ -75,7 +88,7 @@ inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 inline PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
   PagedAttnPlan p;
   const long long group = hq / hkv, rows = n_rows * group, most = max_new * group, n = n_seq;
-  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv, max_len, d) : prompt_shape(rows * hkv, n_rows / n, max_len);
+  p.kg = dtype != SAMKV_BF16 || most <= 32 ? 0 : paged ? paged_shape(most, rows * hkv, max_len, d) : prompt_shape(rows * hkv, n_rows, n, max_len);
   p.once = most <= 32;
   p.target_log2 = p.kg > 0 ? 8 : 9;  // workgroups: as many as are resident at once
   p.min_chunk = p.kg > 0 || (dtype == SAMKV_BF16 && d == 64) ? 256 : 128;  // four waves with a tile of keys each

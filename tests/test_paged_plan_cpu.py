@@ -37,3 +37,12 @@ def test_device_reference_is_the_oracle(n, m):
             k[m - 2, 3] = np.nan
         for a, b in zip(B.attend_rows(q, k, v, 0.4, "cpu"), P.attend_rows(q, k, v, 0.4)):
             assert np.allclose(a, b, rtol=1e-12, atol=1e-14, equal_nan=True), kind
+
+
+def test_sequences_of_padding_do_not_make_prompts_short():
+    """Long prompts in a batch with room for many sequences take wide tiles, as they do alone."""
+    for d in (128, 64):
+        for lens, room in (([8192], 512), ([1024] * 4, 64), ([4000] + [30] * 70, 0), ([2048] * 2, 64)):
+            assert paged_plan.of_prompts("bf16", d, 32, 8, lens + [0] * (room - len(lens)))["kg"] > 0, (d, lens[0], room)
+        # prompts that are short indeed do not: what their tiles cost counts, not their number
+        assert paged_plan.of_prompts("bf16", d, 8, 8, [60] * 8)["kg"] == 0
