@@ -414,9 +414,11 @@ typedef struct {
  *   q, out  n_q_heads of n_tok rows, k, v  n_kv_heads of n_tok rows (out and k, v in dtype); lse float32 [n_q_heads][n_tok], may
  *   be NULL.  cu  device [n_seq + 1]: sequence s is rows cu[s] .. cu[s + 1] - 1.  max_len: bound of the sequences' lengths, rows
  *   of a longer one past the bound are left as they were.
- * This is the prefill that gives the per-document caches of samkv_caches.  Keys and values of later rows do not reach a row
- * whatever they hold (infinities and NaN included; rows beside infinities or NaN among values are computed a second time one by
- * one, which can make a call some hundred times slower).  out must not overlap q, k or v (the same address: SAMKV_EINVAL).
+ * This is the prefill that gives the per-document caches of samkv_caches.  q and k come as they are to be multiplied: a prompt whose
+ * rotary embedding is still to be applied goes into pages by samkv_paged_append, which turns its keys and queries, and attends there
+ * by samkv_paged_attn.  Keys and values of later rows do not reach a row whatever they hold, infinities and NaN included.  Rows whose
+ * tile meets infinities or NaN among values, their own or later ones, are computed a second time one by one: their finite outputs
+ * are as exact, but not bit for bit those of a call without, and the call can become some hundred times slower.  out must not overlap q, k or v (the same address: SAMKV_EINVAL).
  * row_stride of k and v is below 2^24 bytes (SAMKV_EUNSUPPORTED).
  * Arithmetic: scores, maxima, sums and outputs are float32.  float32: products are float32.  bf16: products of bf16 values are
  * exact; a softmax weight enters its product with v rounded to 16 significant bits (two bf16 terms), its sum over the keys being
@@ -445,8 +447,8 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
  *   out[h][t][:] = sum_{j <= p} softmax_j(scale * <q[h][t], K_j[g]>) * V_j[g],  lse[h][t] = log sum_{j <= p} exp(...)
  *   q, out  n_q_heads of n_new rows in the pages' dtype; lse float32 [n_q_heads][n_new], may be NULL.
  * One new token per sequence is a decoding step; several are drafted tokens or a chunk of a prompt; both mix in one batch.
- * A token without a slot attends to nothing: out 0, lse -inf.  Slots behind a token do not reach it whatever they hold.
- * Arithmetic as in samkv_prefill_attn; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long sequences are
+ * A token without a slot attends to nothing: out 0, lse -inf.  Slots behind a token do not reach it whatever they hold, as in
+ * samkv_prefill_attn, and the arithmetic is the same; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long sequences are
  * cut into chunks whose results are joined in float32; which chunks there are follows from the lengths alone.
  * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned; that is enough for every batch of the same pages and heads whose n_seq,
  * n_new, max_new and max_len are no larger, so that a program allocates once for its largest batch (68 MB at most for 8 KV heads of 128, some 110 MB for any). */

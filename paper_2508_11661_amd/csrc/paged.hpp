@@ -74,7 +74,7 @@ struct PagedAttnLaunch {
   float* lse;    // may be null
   float scale;
   int target_log2, ragged_log2;  // workgroups to share the keys out over, and where sequences differ in length
-  int min_chunk;          // no chunk is shorter than min_chunk keys (wide tiles: twice that)
+  int min_chunk;          // keys are shared out in chunks of min_chunk at least (wide tiles: twice that), rounded up to 128
   int max_chunks;         // 1: no sequence's keys are cut
   // partial results of the tiles whose keys are cut, in slots of 32 rows (of tile_rows, where no tile has more)
   int max_slots, tile_rows;

@@ -15,9 +15,10 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
 // ---------------------------------------------------------------------------------------------- few rows
 // A workgroup is NW waves that share one tile of 32 rows and split the keys of their chunk: wave w takes tiles of BK keys w, w
-// + NW, ...  Each wave has its own K and V slot in LDS, filled by asynchronous loads one tile ahead of their use (K of the next
-// tile is requested as soon as K's fragments are in registers, V likewise), so there is no barrier until the waves' results are
-// joined.
+// + NW, ...  Each wave has its own K and V slot in LDS, filled by asynchronous loads (K of the next tile is requested as soon as K's
+// fragments are in registers, V likewise), so there is no barrier until the waves' results are joined.  The first products of a
+// pass do wait for all requests, K of the next tile among them: the compiler cannot see these, and puts its wait for the query
+// fragments, which are loaded before the loop, there.  What overlaps a wave's loads are the other waves.
 // Bound by HBM while each key is read once: 64 sequences x 4096 keys, 32 heads over 8, d = 128: 163 us, 6.6 TB/s (reading 2 GiB: 7.1);
 // one of 131072 keys 86 + 5 us for the join, 6.0 TB/s.  Few short sequences are bound by the chain launch, lengths, page table, K, V,
 // join: 4 x 1000 keys 15 us with the append before it.

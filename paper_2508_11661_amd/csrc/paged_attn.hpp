@@ -154,7 +154,8 @@ struct Items {
         it.q.n = of(q.n);
         it.q.len = of(q.len);
         it.wide = is_wide(it.q);
-        it.c = a.max_chunks > 1 ? ((it.q.len + it.n_chunks - 1) / it.n_chunks + 127) / 128 * 128 : 0x40000000;  // even ones
+        // even chunks, rounded up to 128 keys: the last ones may be short (700 keys in six: five of 128 and one of 60) or empty
+        it.c = a.max_chunks > 1 ? ((it.q.len + it.n_chunks - 1) / it.n_chunks + 127) / 128 * 128 : 0x40000000;
         it.slots = it.wide ? wide_rows<KG>() / 32 : 1;
         it.first_slot = slots_before + of(slots_to - slots);
         const int mine = JOIN ? it.tiles * it.slots : it.tiles * it.n_chunks, local = index - (before + of(upto) - mine);
