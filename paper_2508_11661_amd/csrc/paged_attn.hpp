@@ -24,15 +24,6 @@ __device__ __forceinline__ int scan64(int x) {  // inclusive prefix sum over the
 }
 __device__ __forceinline__ int last_of(int x) { return __builtin_amdgcn_readlane(x, 63); }
 
-// Tiles have 32 rows (KG = 0); or, in launches that have wide ones, sequences of at most 32 rows per KV head are one tile of 32 and
-// the others are cut into wide tiles: KG = 1, 256 rows, KG = 2, 128 rows whose keys two groups of waves share.  So there are no
-// more items than whole tiles in the batch's rows and sequences, and the grid has few workgroups without an item.
-constexpr int kFewRows = 32;
-template <int KG>
-constexpr int wide_rows() { return KG == 2 ? 128 : 256; }
-template <int KG>
-constexpr int wide_cost() { return KG == 2 ? 3 : 5; }  // time of a wide tile over a number of keys, in tiles of 32 rows
-
 struct Item {
   int s;                     // sequence; < 0: no item
   bool wide;
@@ -53,7 +44,7 @@ template <int KG, bool JOIN>
 struct Items {
   const PagedAttnLaunch& a;
   const int lane, group;
-  int c_few, c_wide;              // keys of a chunk
+  ChunkKeys c;                    // keys of a chunk
   int seq, tiles, chunks, slots;  // of this lane's sequence: number, tiles, chunks and partial results
   SeqSpan q;
   int upto, slots_to;             // items (or groups of rows) and partial results up to it in its block of 64
@@ -71,7 +62,7 @@ struct Items {
   }
   __device__ __forceinline__ void count() {
     const int per = is_wide(q) ? wide_rows<KG>() / 32 : 1;
-    chunks = a.max_chunks > 1 ? max(is_wide(q) ? (q.len + c_wide / 4) / c_wide : (q.len + c_few - 1) / c_few, 1) : 1;
+    chunks = a.max_chunks > 1 ? chunks_of(is_wide(q), q.len, c) : 1;
     slots = chunks > 1 ? tiles * chunks * per : 0;
     upto = scan64(JOIN ? (chunks > 1 ? tiles * per : 0) : tiles * chunks);
     slots_to = a.max_chunks > 1 ? scan64(slots) : 0;
@@ -79,7 +70,7 @@ struct Items {
 
   __device__ __forceinline__ Items(const PagedAttnLaunch& a_) : a(a_), lane(threadIdx.x & 63), group(a_.hq / a_.hkv) {
     read(0);
-    c_few = c_wide = 0;
+    c = {};
     if (a.max_chunks > 1) {
       // keys of a chunk of 32 rows: the cost of all tiles and heads over the number of workgroups (2^target_log2); a wide tile's
       // are fewer by what it costs more
@@ -98,13 +89,7 @@ struct Items {
       // sequences of one length make chunks of one length, and as many workgroups as are resident end together; others do not,
       // and half as long ones leave less at the end (64 sequences, 1024 to 8192 keys, 8 heads: 222 -> 204 us; all of 4096: 168 and 175)
       const bool uneven = a.ragged_log2 > a.target_log2 && __any((float)longest * (float)last_of(scan64(n)) > 1.25f * (float)total);
-      const int log2 = uneven ? a.ragged_log2 : a.target_log2;
-      const int share = (int)min((total * a.hkv + (1ull << log2) - 1) >> log2, 0x40000000ull);
-      c_few = max((share + 63) / 64 * 64, a.min_chunk);
-      // Wide tiles fill a compute unit and spend the time of 500 keys on their start and end: no more of them than there are units,
-      // so a sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 62 us
-      // with chunks rounded up, 46 to the nearest, 42 uncut; 500 over 8000, 128 tiles: 118 either way, 151 uncut).
-      c_wide = max(share / wide_cost<KG>(), 2 * a.min_chunk);
+      c = chunk_keys<KG>(total, a.hkv, uneven ? a.ragged_log2 : a.target_log2, a.min_chunk);
     }
     if (KG > 0 && a.paged && a.b.n_seq > 1 && a.b.n_seq <= 64) {
       int rank = 0;

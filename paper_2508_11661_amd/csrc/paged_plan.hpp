@@ -16,6 +16,35 @@ struct PagedAttnPlan {
   size_t part_lse, bytes;  // workspace: part_o, then part_lse
 };
 
+// Tiles have 32 rows (KG = 0); or, in launches that have wide ones, sequences of at most 32 rows per KV head are one tile of 32 and
+// the others are cut into wide tiles: KG = 1, 256 rows, KG = 2, 128 rows whose keys two groups of waves share.  So there are no
+// more items than whole tiles in the batch's rows and sequences, and the grid has few workgroups without an item.
+constexpr int kFewRows = 32;
+template <int KG>
+constexpr int wide_rows() { return KG == 2 ? 128 : 256; }
+template <int KG>
+constexpr int wide_cost() { return KG == 2 ? 3 : 5; }  // time of a wide tile over a number of keys, in tiles of 32 rows
+
+
+// What the device makes of a batch's lengths (Items in paged_attn.hpp).  Keys of a chunk: the cost of all tiles and heads, `total` keys
+// of tiles of 32 rows, is shared out over 2^log2 workgroups; a wide tile's chunk has fewer keys by what the tile costs more.
+// Wide tiles fill a compute unit and spend the time of 500 keys on their start and end: no more of them than there are units, so a
+// sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 62 us with
+// chunks rounded up, 46 to the nearest, 42 uncut; 500 over 8000, 128 tiles: 118 either way, 151 uncut).
+struct ChunkKeys {
+  int few, wide;
+};
+template <int KG>
+constexpr ChunkKeys chunk_keys(unsigned long long total, int hkv, int log2, int min_chunk) {
+  const unsigned long long share = (total * hkv + (1ull << log2) - 1) >> log2, of_wide = share / wide_cost<KG>(), longest = 1ull << 30;
+  const int few = (int)((share < longest ? share : longest) + 63) / 64 * 64, wide = (int)(of_wide < longest ? of_wide : longest);
+  return {few > min_chunk ? few : min_chunk, wide > 2 * min_chunk ? wide : 2 * min_chunk};
+}
+constexpr int chunks_of(bool wide, int len, ChunkKeys c) {
+  const int n = wide ? (len + c.wide / 4) / c.wide : (len + c.few - 1) / c.few;
+  return n > 1 ? n : 1;
+}
+
 // Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not
 // full), with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the
 // smaller), one and a half for tiles of 32 rows, of which two share one.
