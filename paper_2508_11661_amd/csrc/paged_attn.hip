@@ -233,13 +233,13 @@ __global__ __launch_bounds__(256, 2) void k_attend_few(PagedAttnLaunch a) {
 // The running maximum is raised only when a row outgrows it by 2^8, which keeps the rescaling of O off the common path: weights
 // stay below 256.  A weight is the sum of two bf16 terms (16 significant bits), each multiplied by V, as in attend_few: a token's
 // error is that of its output's rounding, whatever batch it comes in.  One term (half a step, 2^-8 relative) would take two matrix
-// products per key instead of three, 4.4 ms instead of 6.0 for 16 prompts of 4096 tokens, 64 heads over 8, but doubles the squared
+// products per key instead of three, 4.3 ms instead of 5.7 for 16 prompts of 4096 tokens, 64 heads over 8, but doubles the squared
 // error of the outputs (2.2e-3 of their norm instead of 1.6e-3).  The sum is that of the unrounded weights, in float32.
 // KG = 1: 256 rows and 64 keys a step, tiles requested two steps ahead.  KG = 2, where 256 rows at a time would leave compute
 // units idle or the longest tile's chain of steps would last: 128 rows, and 128 keys a step of which either half of the waves
 // takes 64; the halves meet through LDS at the end.
-// Bound by the power limit.  One prompt of 24000 tokens, 32 heads over 8: d = 128 780 TFLOP/s of the operator, 1170 of the matrix
-// unit; d = 64 630; 16 of 1024 tokens 510: a workgroup's start and end (lengths, first K tile, queries, output rows) take as long as
+// Bound by the power limit.  One prompt of 24000 tokens, 32 heads over 8: d = 128 824 TFLOP/s of the operator, 1240 of the matrix
+// unit; d = 64 664; 10 of 1024 tokens 520: a workgroup's start and end (lengths, first K tile, queries, output rows) take as long as
 // three steps of a mean of 8.5.  Measured with one-term weights: two workgroups of 128 rows and four waves per compute unit, whose starts
 // and ends overlap, read K and V twice as often: 16 x 1024 217 -> 203 us, but 23 of 580 to 2999 tokens 813 -> 817, 1 x 8000 498 -> 514,
 // chunks over pages up to 8 % slower.
@@ -458,10 +458,12 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
     auto step = [&](f32x16 (&sc)[2], f32x16 (&sn)[2], auto kind) {
       constexpr bool masked = kind.value;
       constexpr int NS = 2 * ND, NP = 8 * NV, RV = 4;  // products of S and of O, fragments of V that are here
-      constexpr int FIRST = 4, UNDER_S = 4;    // pairs of weights made ahead of the products and under those of S
+      constexpr int FIRST = 2, UNDER_S = 6, LATE = 16 - FIRST - UNDER_S;  // pairs of weights made ahead of the products, under S, under O
+      static_assert(FIRST + UNDER_S >= 8, "the weights of two groups of 16 keys are here before O's first product, the others in time");
       uint32_t ks = k_at + s1, vs = v_at + s0;
       asm volatile("" : "+v"(ks), "+v"(vs));
-      bf16x8 ak[ND], hi[4], lo[4];
+      bf16x8 ak[ND];
+      Frag hi[4], lo[4];
       Frag va[RV];
       float psum = 0.f;
       auto k_read = [&](int i) {
@@ -480,10 +482,12 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
         const int g = k / 4, e = 2 * (k % 4);
         const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e], c2, -m_use));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[g >> 1][8 * (g & 1) + e + 1], c2, -m_use));
-        hi[g][e] = (__bf16)p0;
-        hi[g][e + 1] = (__bf16)p1;
-        lo[g][e] = (__bf16)(p0 - (float)hi[g][e]);
-        lo[g][e + 1] = (__bf16)(p1 - (float)hi[g][e + 1]);
+        const bf16x2 first = {(__bf16)p0, (__bf16)p1};
+        uint32_t both = __builtin_bit_cast(uint32_t, first);
+        asm("" : "+v"(both));  // taken apart as they lie: the compiler would convert them again, one by one
+        const bf16x2 second = {(__bf16)(p0 - bf16_lo(both)), (__bf16)(p1 - bf16_hi(both))};
+        hi[g].u[e / 2] = both;
+        lo[g].u[e / 2] = __builtin_bit_cast(uint32_t, second);
         psum += p0 + p1;
         asm volatile("" : : "v"(psum));  // here, not where the sum is used
       };
@@ -508,9 +512,9 @@ __device__ __forceinline__ void attend_wide(const PagedAttnLaunch& a, const Item
 #pragma unroll
       for (int j = 0; j < NP; ++j) {
         const int f = j / 2, g = f / NV;  // fragment of V, its 16 keys
-        o[f % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[f % RV].b, j % 2 == 0 ? hi[g] : lo[g], o[f % NV], 0, 0, 0);
+        o[f % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[f % RV].b, j % 2 == 0 ? hi[g].b : lo[g].b, o[f % NV], 0, 0, 0);
         if (j % 2 != 0 && f + RV < 4 * NV) v_read(f + RV);
-        constexpr int LATE = 16 - FIRST - UNDER_S, EARLY = NP / 2, MAXES = (32 / (NP - EARLY) + 2) / 2 * 2;  // maxima: one instruction takes two
+        constexpr int EARLY = NP / 2, MAXES = (32 / (NP - EARLY) + 2) / 2 * 2;  // maxima: one instruction takes two
         if (j < EARLY) {
           if ((j + 1) * LATE / EARLY > j * LATE / EARLY) pair(FIRST + UNDER_S + j * LATE / EARLY);
         } else if constexpr (!masked) {
