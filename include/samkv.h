@@ -418,7 +418,8 @@ typedef struct {
  * rotary embedding is still to be applied goes into pages by samkv_paged_append, which turns its keys and queries, and attends there
  * by samkv_paged_attn.  Keys and values of later rows do not reach a row whatever they hold, infinities and NaN included.  Rows whose
  * tile meets infinities or NaN among values, their own or later ones, are computed a second time one by one: their finite outputs
- * are as exact, but not bit for bit those of a call without, and the call can become some hundred times slower.  out must not overlap q, k or v (the same address: SAMKV_EINVAL).
+ * are as exact, but not bit for bit those of a call without, and the call can become some hundred times slower.  out must not
+ * overlap q, k or v (the same address: SAMKV_EINVAL).
  * row_stride of k and v is below 2^24 bytes (SAMKV_EUNSUPPORTED).
  * Arithmetic: scores, maxima, sums and outputs are float32.  float32: products are float32.  bf16: products of bf16 values are
  * exact; a softmax weight enters its product with v rounded to 16 significant bits (two bf16 terms), its sum over the keys being

@@ -37,8 +37,8 @@ struct Item {
 // Finds work items: JOIN = false, number `index` of them; JOIN = true, group of 32 rows number `index` among the tiles whose keys
 // are cut (the chunk is the first).  All calls are by whole waves, and the results are the same in every lane.  A lane holds one of
 // 64 sequences; batches of up to that many are read once, and over a cache wide tiles are taken in order of falling length, so that
-// a long sequence's are not the last to start (24 sequences with 1 to 1024 new tokens, those with many in front: 549 us either way,
-// at the end: 610 -> 520; prompts gain less than the order costs, 2 %).  Within a sequence items run chunk by chunk, the last tile
+// a long sequence's are not the last to start (24 sequences with 1 to 1024 new tokens, those with many in front: 532 -> 525 us, at
+// the end: 587 -> 483; prompts gain less than the order costs, 2 %).  Within a sequence items run chunk by chunk, the last tile
 // (with the most keys) first.
 template <int KG, bool JOIN>
 struct Items {

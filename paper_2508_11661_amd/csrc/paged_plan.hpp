@@ -29,8 +29,8 @@ constexpr int wide_cost() { return KG == 2 ? 3 : 5; }  // time of a wide tile ov
 // What the device makes of a batch's lengths (Items in paged_attn.hpp).  Keys of a chunk: the cost of all tiles and heads, `total` keys
 // of tiles of 32 rows, is shared out over 2^log2 workgroups; a wide tile's chunk has fewer keys by what the tile costs more.
 // Wide tiles fill a compute unit and spend the time of 500 keys on their start and end: no more of them than there are units, so a
-// sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 62 us with
-// chunks rounded up, 46 to the nearest, 42 uncut; 500 over 8000, 128 tiles: 118 either way, 151 uncut).
+// sequence's chunks are rounded to the nearest, down up to 3/4 (2 x 300 tokens over 1500 keys, 32 heads, 160 tiles: 59 us with
+// chunks rounded up, 44 to the nearest, 39 uncut; 500 over 8000, 128 tiles: 108 either way, 151 uncut).
 struct ChunkKeys {
   int few, wide;
 };
@@ -45,18 +45,18 @@ constexpr int chunks_of(bool wide, int len, ChunkKeys c) {
   return n > 1 ? n : 1;
 }
 
-// Which tiles a batch takes (KG).  Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not
-// full), with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the
-// smaller), one and a half for tiles of 32 rows, of which two share one.
-// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are.  Measured, prompts of one length,
-// tiles of 32 / 128 / 256 rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 15 / 16, 1 x 1000 36 / 31 / 44, 1 x 2048 97 / 68
-// / 85, 1 x 4096 315 / 231 / 210, 4 x 512 49 / 38 / 33, 32 x 64 29 / 22 / 15, 20 x 300 102 / 82 / 58; d = 64, 8 heads: 1 x 1000 12
-// / 20 / 30, 1 x 2048 20 / 32 / 51, 1 x 4096 50 / 58 / 96, 10 x 700 31 / 32 / 24.
+// Which tiles a batch takes (KG). Times of a workgroup in steps of 256 rows x 64 keys (about 2.8 us, 2 where the chip is not full),
+// with what it spends on its start and end: four steps for the wide kernels, which fill a compute unit each (five for the smaller),
+// one and a half for tiles of 32 rows, of which two share one.
+// Prompts: the larger of the longest workgroup and the mean one times the rounds that there are. Measured, prompts of one length,
+// tiles of 32 / 128 / 256 rows, us: d = 128, 32 heads over 8: 1 x 200 tokens 10 / 14 / 16, 1 x 1000 35 / 31 / 42, 1 x 2048 95 / 65
+// / 81, 1 x 4096 314 / 226 / 207, 4 x 512 49 / 37 / 31, 32 x 64 29 / 22 / 15, 20 x 300 101 / 81 / 57; d = 64, 8 heads: 1 x 1000 12
+// / 19 / 28, 1 x 2048 19 / 31 / 49, 1 x 4096 51 / 56 / 91, 10 x 700 31 / 31 / 24.
 // How the rows are spread over the sequences is known to the device alone: anything from evenly over all of them to prompts of
 // max_len beside sequences of padding (a captured batch with room for many), so the tiles are taken whose loss is smallest where it
-// is largest.  32 heads over 8, d = 128, 32 / 128 / 256 rows, us: 1 x 4000 tokens beside 70 x 30 363 / 277 / 237, 1 x 8192 and 511
-// sequences without rows 1108 / 857 / 798, 4 x 1024 and 60 without 112 / 78 / 79; 8 heads over 2: 83 / 81 / 130, 280 / 221 / 282,
-// 37 / 29 / 42.
+// is largest. 32 heads over 8, d = 128, 32 / 128 / 256 rows, us: 1 x 4000 tokens beside 70 x 30 348 / 253 / 222, 1 x 8192 and 511
+// sequences without rows 1060 / 814 / 753, 4 x 1024 and 60 without 110 / 79 / 78; 8 heads over 2: 80 / 80 / 122, 268 / 210 / 263,
+// 36 / 28 / 40.
 inline int prompt_shape(long long rows, long long n_rows, long long n_seq, int max_len) {
   struct Times { double few, wide, mid; };
   auto times = [&](double mean_len) {
@@ -75,12 +75,12 @@ inline int prompt_shape(long long rows, long long n_rows, long long n_seq, int m
   return few <= wide && few <= mid ? 0 : wide <= mid ? 1 : 2;
 }
 // New tokens over a cache: tiles of 32 rows where they are few (`tiles`, of all heads) and have few keys to see, since two of them
-// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many.  Measured, 32 / 128 / 256
-// rows, us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 14.7 / 21.2 / 29.9, 4 x 128 19.4 / 22.7 / 30.3, 16 x 64 36 / 26
-// / 33, 64 x 40 78 / 93 / 69; over 2000: 1 x 64 19.5 / 28.0 / 34, 4 x 128 42 / 48 / 50, 4 x 400 118 / 93 / 83; over 6000: 1 x 64 32
-// / 37 / 49, 1 x 256 69 / 55 / 57; 8 heads over 2, d = 64: 4 x 400 over 2000 28 / 34 / 34, 16 x 64 24 / 31 / 34, 16 x 200 51 / 39 /
-// 60, over 6000: 4 x 400 73 / 60 / 59.  Sequences of at most two tiles of 32 have less to gain from sharing keys, 32 heads over 8,
-// d = 128: 64 x 16 over 600 39 / 50 / 50, over 2000 123 / 129 / 129, over 6000 309 / 303 / 303, 16 x 16 over 6000 90 / 95 / 95.
+// share a compute unit and start and end in half the time; else 128 rows, or 256 where there are many. Measured, 32 / 128 / 256
+// rows, us, 32 heads over 8, d = 128: 1 x 256 tokens over 600 keys 16 / 21 / 29, 4 x 128 21 / 22 / 30, 16 x 64 38 / 26 / 33, 64 x
+// 40 83 / 93 / 68; over 2000: 1 x 64 19 / 27 / 33, 4 x 128 43 / 46 / 50, 4 x 400 120 / 90 / 80; over 6000: 1 x 64 31 / 37 / 46, 1 x
+// 256 84 / 53 / 57; 8 heads over 2, d = 64: 4 x 400 over 2000 27 / 34 / 34, 16 x 64 24 / 33 / 34, 16 x 200 51 / 38 / 58, over 6000:
+// 4 x 400 70 / 58 / 57. Sequences of at most two tiles of 32 have less to gain from sharing keys, 32 heads over 8, d = 128: 64 x 16
+// over 600 41 / 50 / 51, over 2000 120 / 123 / 122, over 6000 306 / 304 / 306, 16 x 16 over 6000 90 / 94 / 95.
 inline int paged_shape(long long most, long long rows, int max_len, int d) {
   const double tiles = rows / 32.0, keys = tiles * max_len;
   if (most <= 64 ? keys <= 2.6e6 : tiles <= 512 && keys * d <= 8e5 * 128) return 0;
@@ -89,12 +89,12 @@ inline int paged_shape(long long most, long long rows, int max_len, int d) {
 
 // Whether the keys of a batch over pages may be cut: where the longest sequence can take `passes` steps of a tile's keys, `share`
 // of the compute units have a tile without that, and the join (4 us; 6 to 10 for the results of wide tiles) costs less than the
-// other units save.  Where they all have one, only sequences of very different lengths gain, which the host does not see, and long
-// ones are cut so that none takes the time of many.  Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4
-// sequences of 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to
-// 2000 59 / 61, 375 to 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 2 x 300 tokens over 1500 39.0 / 43.7, 8 x 200 over 3000 118
-// / 127, 1 x 500 over 2000 47.5 / 46.5, 3000 63 / 56, 8000 151 / 110, 16 x 64 over 400 to 3000 69 / 72, 750 to 6000 124 / 114; 32 x
-// 100, one over 30000 keys and the others over 600: 950 / 171.
+// other units save. Where they all have one, only sequences of very different lengths gain, which the host does not see, and long
+// ones are cut so that none takes the time of many. Measured, uncut / cut, us: single tokens, d = 128, 32 heads over 8: 4 sequences
+// of 380 keys 14.3 / 14.7, 500 15.5 / 14.7, 16 of 760 20.6 / 21.2, 1000 24.4 / 22.3, 24 of 2000 42 / 47, 64 of 250 to 2000 59 / 61,
+// 375 to 3000 83 / 82, 500 to 4000 111 / 106; wide tiles: 2 x 300 tokens over 1500 37 / 42, 8 x 200 over 3000 119 / 121, 1 x 500
+// over 2000 44 / 44, 3000 61 / 54, 8000 143 / 108, 16 x 64 over 400 to 3000 66 / 68, 750 to 6000 117 / 111; 32 x 100, one over
+// 30000 keys and the others over 600: 917 / 161.
 inline bool cuts(int kg, double share, double passes) {
   if (kg > 0) return passes > (share <= 0.5 ? 8 / (1 - share) : 32);
   return passes > (share < 1 && 3 / (1 - share) < 16 ? 3 / (1 - share) : 16);
