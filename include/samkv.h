@@ -449,10 +449,11 @@ int samkv_paged_append(const samkv_pages* pages, const samkv_batch* batch, const
  *   q, out  n_q_heads of n_new rows in the pages' dtype; lse float32 [n_q_heads][n_new], may be NULL.
  * One new token per sequence is a decoding step; several are drafted tokens or a chunk of a prompt; both mix in one batch.
  * A token without a slot attends to nothing: out 0, lse -inf.  Slots behind a token do not reach it whatever they hold, as in
- * samkv_prefill_attn, and the arithmetic is the same; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long sequences are
- * cut into chunks whose results are joined in float32; which chunks there are follows from the lengths alone.
- * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned; that is enough for every batch of the same pages and heads whose n_seq,
- * n_new, max_new and max_len are no larger, so that a program allocates once for its largest batch (68 MB at most for 8 KV heads of 128, some 110 MB for any). */
+ * samkv_prefill_attn, and the arithmetic is the same; out must not overlap q (the same address: SAMKV_EINVAL).  The keys of long
+ * sequences are cut into chunks whose results are joined in float32; which chunks there are follows from the lengths alone.
+ * ws: samkv_paged_workspace_bytes(...) bytes, 256-byte aligned; that is enough for every batch of the same pages and heads whose
+ * n_seq, n_new, max_new and max_len are no larger, so that a program allocates once for its largest batch (68 MB at most for 8 KV
+ * heads of 128 channels, some 110 MB for any). */
 size_t samkv_paged_workspace_bytes(const samkv_pages* pages, const samkv_batch* batch, int32_t n_q_heads);
 int samkv_paged_attn(const samkv_pages* pages, const samkv_batch* batch, const samkv_rows* q, int32_t n_q_heads, float scale,
                      const samkv_rows* out, float* lse, void* ws, size_t ws_bytes, void* stream);

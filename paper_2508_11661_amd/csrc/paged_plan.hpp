@@ -111,7 +111,7 @@ inline long long shares_of(int log2, int hkv) { return ((1 << log2) + hkv - 1) /
 inline long long slots_of(long long tiles, long long shares, long long tile) {
   return (tiles + shares < 2 * shares ? tiles + shares : 2 * shares) * (tile / 32);
 }
-constexpr int kUneven = 10;  // target_log2 and ragged_log2 of tiles of 32 rows: at most
+constexpr int kUneven = 10;  // ragged_log2 of tiles of 32 rows
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 inline PagedAttnPlan paged_attn_plan(int dtype, int d, int hq, int hkv, int n_seq, int n_rows, int max_new, int max_len, bool paged) {
